@@ -1,0 +1,71 @@
+/* C ABI of the 8-bit integer operators, and of the Encode stage that runs its products on them.
+ *
+ * A tensor in 8 bits is a matrix of codes, dev int8, with a float32 scale per row: code c of row r stands for
+ * c * scale[r].  Rows are tokens (activations) or output channels (weights, stored [out][in] as everywhere in this
+ * library), so that a product of the two needs one factor per result.  Codes lie in -127 .. 127:
+ *     scale = max(max|row| / 127, 2^-126)     (float32, rounded to nearest)
+ *     code  = value / scale                   (rounded to nearest, ties to even, of the exact quotient)
+ * A row of zeros has codes 0.  A row that holds an infinity or a NaN has codes 0 and the scale NaN: what is computed
+ * from it is NaN, and other rows are not touched.
+ *
+ * Conventions are those of dit.h: status codes, caller-owned device buffers, nothing allocated, arguments
+ * checked before anything is launched, launches only (no copies, no waiting: every dit_op_* call here may be captured into a HIP
+ * graph), on `stream` (NULL = default stream) of the current device.  Buffers and matrix rows start at multiples of 16 bytes
+ * (scales, gains, biases, gates and maps: at their element's size).  Buffers of one call do not overlap unless it says so.
+ */
+#ifndef DIT_INT8_H
+#define DIT_INT8_H
+
+#include "encoder.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { DIT_X_BF16 = 0, DIT_X_F32 = 1 };
+enum { DIT_I8_MAX_ROW = 16384, /* columns of a row that gets codes */
+       DIT_I8_MAX_K = 131072 - 128 /* K of a product: its sums stay inside 32 bits */ };
+
+/* Codes and scales of the rows of x [M][ldx], d columns each (1..DIT_I8_MAX_ROW, any number), x_kind DIT_X_*.
+ * codes: [M][ldq], ldq at least d rounded up to 128: the columns from d to there are set to 0, which makes the row an
+ * operand of a product with K = d rounded up to 128. */
+dit_status dit_op_quantize_i8(void* stream, const void* x, int x_kind, int ldx, int M, int d, void* codes, int ldq, float* scale);
+
+/* RMS norm with the residual's addition, leaving codes:
+ *     x' = x + delta;   y = x' / sqrt(mean(x'^2) + eps) * gain;   codes and scales of the rows y (never rounded before).
+ * x: dev float32 [M][ldx]; delta: [M][ldd], delta_kind DIT_X_*, NULL = none; x_out: dev float32 [M][ldo] receives x', may be x
+ * itself (with ldo == ldx) or NULL; gain: dev float32 [d], 16-byte aligned; eps > 0; codes and columns past d as above.  The statistics are held in 64 bits, so
+ * that codes and scales are those of the formulas whatever the order of the sums. */
+dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* delta, int delta_kind, int ldd, const float* gain,
+                             float eps, int M, int d, float* x_out, int ldo, void* codes, int ldq, float* scale);
+
+/* C[m][n] = a_scale[m] * w_scale[n] * sum_k A[m][k] W[n][k] (+ bias[n]) on the 8-bit matrix cores; the sum is exact.
+ * A: codes [M][lda]; W: codes [N][ldw] (no padding rows needed); a_scale: dev float32 [M]; w_scale: dev float32 [N]; bias: dev float32
+ * [N] or NULL; K a multiple of 128, at most DIT_I8_MAX_K; lda, ldw multiples of 16 below 2^22.  out_kind, out, ldc, gate, gate_stride and row_req
+ * as for dit_op_gemm (0 bf16, 1 float32, 2 bf16 of tanh-GELU, 3 float32 out += gate * C); any code -128..127 is
+ * taken.  The result does not depend on how the product is cut up: it is the same, bit for bit, alone or among other rows.
+ * work: dev scratch for the shares of a product split along K, may be NULL (not split); dit_op_gemm_i8_work_bytes
+ * says how much the library's choice uses, less makes fewer shares.  Its contents carry nothing between calls; calls that
+ * may overlap need one each. */
+dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_scale, const void* W, int ldw, const float* w_scale,
+                          const float* bias, int M, int N, int K, int out_kind, void* out, int ldc, const float* gate,
+                          int gate_stride, const int* row_req, void* work, size_t work_bytes);
+
+/* bf16 of tanh-GELU(product with W_gate) * (product with W_up), both [N][ldw]. */
+dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const float* a_scale, const void* W_gate, const float* gate_scale,
+                                const void* W_up, const float* up_scale, int ldw, int M, int N, int K, void* out, int ldc,
+                                void* work, size_t work_bytes);
+
+/* bf16 of the product (+ bias), element (m, n) to out[n*ldo + col[m]]; col: dev int32 [M], rising, below ldo; columns that no
+ * row maps to are left alone. */
+dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const float* a_scale, const void* W, int ldw,
+                                     const float* w_scale, const float* bias, int M, int N, int K, void* out, int ldo,
+                                     const int* col, void* work, size_t work_bytes);
+
+/* Scratch of one such call (pair != 0: dit_op_gemm_i8_geglu); 0 where nothing is split or the arguments are refused. */
+size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

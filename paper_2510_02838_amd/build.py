@@ -7,7 +7,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdit.so")
-SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "encoder.hip", "decoder.hip", "dit_api.cpp", "enc_api.cpp", "dec_api.cpp", "dispatch.cpp"]
+SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "encoder.hip", "decoder.hip", "dit_api.cpp", "enc_api.cpp", "dec_api.cpp", "dispatch.cpp",
+           "int8.hip", "gemm_i8.hip", "int8_api.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

@@ -1,0 +1,514 @@
+"""The 8-bit integer operators through the C ABI, against their formulas in 64 bits.
+
+A rounding to float32 is off by at most 2^-24 of the value, one to bf16 by 2^-8.  Codes and scales are compared as they are:
+the scale is one rounded quotient, a code the rounding of an exact one.
+"""
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+F32, BF16 = 2.0 ** -24, 2.0 ** -8
+TINY = 2.0 ** -126
+
+
+@pytest.fixture(scope="module")
+def Q():
+    from paper_2510_02838_amd import int8
+    return int8
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    torch.cuda.set_device(0)
+    return torch
+
+
+def up(n, a):
+    return -(-n // a) * a
+
+
+# ------------------------------------------------------------------------------------------------ host logic
+def test_library_exports_every_declared_symbol(Q):
+    hdr = open(os.path.join(ROOT, "include", "int8.h")).read()
+    hdr = re.sub(r"/\*.*?\*/", "", hdr, flags=re.S)
+    assert set(re.findall(r"\b((?:dit_op|enc_i8)_[a-z_0-9]+)\s*\(", hdr)) == set(Q.EXPORTS)
+
+
+def test_row_operators_check_their_arguments(Q):
+    """(Addresses are never dereferenced.)"""
+    quant = lambda x=256, kind=0, ldx=128, M=4, d=100, codes=256, ldq=128, scale=256: Q.dit_op_quantize_i8(None, x, kind, ldx, M, d, codes, ldq, scale)  # noqa: E731
+    assert quant(x=None) == quant(codes=None) == quant(scale=None) == quant(kind=2) == 1
+    assert quant(M=-1) == quant(d=0) == quant(d=16385, ldx=16392, ldq=16512) == quant(ldx=96) == quant(ldx=100) == quant(ldq=112) == quant(ldq=136) == 2
+    assert quant(kind=1, ldx=102) == quant(x=264) == quant(codes=264) == 2
+    assert quant(M=0) == 0
+    norm = lambda x=256, ldx=128, delta=256, dk=0, ldd=128, gain=256, eps=1e-6, M=4, d=100, xo=256, ldo=128, codes=256, ldq=128, scale=256: (  # noqa: E731
+        Q.dit_op_rmsnorm_i8(None, x, ldx, delta, dk, ldd, gain, eps, M, d, xo, ldo, codes, ldq, scale))
+    assert norm(x=None) == norm(gain=None) == norm(codes=None) == norm(scale=None) == norm(dk=5) == 1
+    assert norm(eps=0.0) == norm(eps=-1.0) == norm(eps=math.nan) == norm(eps=math.inf) == 1
+    assert norm(M=-1) == norm(d=0) == norm(d=16385, ldx=16388, ldd=16392, ldo=16388, ldq=16512) == norm(ldx=96) == norm(ldx=102) == norm(ldq=112) == 2
+    assert norm(ldd=96) == norm(ldd=100) == norm(delta=264) == norm(ldo=96) == norm(xo=264) == norm(ldo=132) == norm(x=264) == norm(gain=260) == 2
+    assert norm(M=0) == norm(M=0, delta=None, dk=9, xo=None) == norm(M=0, xo=512, ldo=132) == 0
+
+
+def test_products_check_their_arguments(Q):
+    plain = lambda A=256, lda=128, sa=256, W=256, ldw=128, sw=256, M=4, N=8, K=128, kind=0, out=256, ldc=8, work=None, n=0: (  # noqa: E731
+        Q.dit_op_gemm_i8(None, A, lda, sa, W, ldw, sw, None, M, N, K, kind, out, ldc, None, 0, None, work, n))
+    pair = lambda up=256, us=256, ld=128, N=8, ldc=8, out=256, M=4: (  # noqa: E731
+        Q.dit_op_gemm_i8_geglu(None, 256, 128, 256, 256, 256, up, us, ld, M, N, 128, out, ldc, None, 0))
+    tr = lambda col=256, ldo=8, out=256, M=4: Q.dit_op_gemm_i8_transposed(None, 256, 128, 256, 256, 128, 256, None, M, 8, 128, out, ldo, col, None, 0)  # noqa: E731
+    assert plain(A=None) == plain(sa=None) == plain(W=None) == plain(sw=None) == plain(out=None) == plain(kind=4) == plain(kind=-1) == 1
+    assert plain(K=0) == plain(K=64) == plain(K=192, lda=256, ldw=256) == plain(K=131072, lda=131072, ldw=131072) == plain(K=256) == 2
+    assert plain(lda=136) == plain(ldw=136) == plain(lda=1 << 22) == plain(ldw=1 << 22) == plain(M=-1) == plain(N=-1) == 2
+    assert plain(ldc=4) == plain(ldc=12) == plain(N=5, kind=1, ldc=6) == plain(A=264) == plain(W=264) == plain(out=264) == plain(work=264, n=1 << 20) == 2
+    assert plain(M=0) == plain(N=0) == pair(M=0) == tr(M=0) == 0
+    assert pair(up=None) == pair(us=None) == 1 and pair(up=264) == pair(ld=112) == pair(ldc=12) == pair(ldc=0) == 2
+    assert tr(col=None) == 1 and tr(ldo=0) == tr(ldo=12) == tr(out=264) == 2
+    assert Q.dit_op_gemm_i8_work_bytes(0, 8, 128, 0) == Q.dit_op_gemm_i8_work_bytes(4, 8, 100, 0) == Q.dit_op_gemm_i8_work_bytes(4, 8, 131072, 0) == 0
+    with pytest.raises(Exception, match="DIT_ESHAPE"):
+        Q.check(2)
+
+
+# ------------------------------------------------------------------------------------------------ rows to codes
+def codes_of(y):
+    """Scales and exact quotients of float64 rows."""
+    s = np.maximum((np.abs(y).max(axis=1) / 127.0).astype(np.float32), np.float32(TINY))
+    return s, y / s[:, None].astype(np.float64)
+
+
+def run_quantize(torch, Q, x, d, ldq=None, stream=None):
+    M, ldq = x.shape[0], ldq or up(d, 128)
+    codes = torch.full((M, ldq), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((M,), -1.0, device="cuda")
+    Q.check(Q.dit_op_quantize_i8(stream, x.data_ptr(), int(x.dtype == torch.float32), x.stride(0), M, d, codes.data_ptr(), ldq, scale.data_ptr()))
+    torch.cuda.synchronize()
+    return codes.cpu().numpy(), scale.cpu().numpy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,d,pad", [(1, 1, 0), (3, 7, 8), (5, 64, 0), (9, 129, 16), (2, 255, 0), (1, 256, 0), (7, 1000, 24), (4, 1024, 0), (3, 1025, 0), (33, 2050, 8),
+                                     (2, 4096, 0), (5, 4100, 0), (2, 8192, 8), (3, 8193, 0), (2, 10240, 0), (3, 16384, 0), (1000, 333, 0)])
+def test_quantize_is_the_rounded_quotient(torch, Q, dtype, M, d, pad):
+    g = torch.Generator().manual_seed(M * 7919 + d)
+    x = torch.randn(M, up(d, 8) + pad, generator=g) * torch.exp(3 * torch.randn(M, 1, generator=g))
+    if M > 2:
+        x[1] = 0.0                                                   # a row of zeros
+        x[2, :d] = torch.round(x[2, :d] * 20) * 0.75                 # many exact ties: the scale is 0.75 where the largest is 127 * 0.75
+        x[2, 0] = 127 * 0.75
+        x[2, 1:d] = x[2, 1:d].clamp(-127 * 0.75, 127 * 0.75) + (0.375 if d > 1 else 0)
+        x[2, 1:d] = x[2, 1:d].clamp(-127 * 0.75, 127 * 0.75)
+    x = x.cuda().to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    ldq = up(d, 128) + 16
+    codes, scale = run_quantize(torch, Q, x, d, ldq)
+    s, q = codes_of(x[:, :d].double().cpu().numpy())
+    assert np.array_equal(scale, s)
+    assert np.array_equal(codes[:, :d], np.rint(q).astype(np.int8))
+    assert not codes[:, d:up(d, 128)].any() and (codes[:, up(d, 128):] == 77).all()
+
+
+@pytest.mark.gpu
+def test_quantize_of_extreme_rows(torch, Q):
+    """Infinities and NaN stay in their rows; the smallest and the largest numbers keep their codes."""
+    x = torch.randn(8, 512, generator=torch.Generator().manual_seed(3)).cuda()
+    x[0, 17], x[1, 500], x[2, 0], x[3, 3] = math.inf, -math.inf, math.nan, -math.nan
+    x[4] *= 1e-44
+    x[5] *= 8e37
+    x[6] = 0.0
+    x[6, 5] = -1e-45
+    codes, scale = run_quantize(torch, Q, x, 512)
+    assert np.isnan(scale[:4]).all() and not codes[:4].any()
+    s, q = codes_of(x[4:].double().cpu().numpy())
+    assert np.array_equal(scale[4:], s) and np.array_equal(codes[4:], np.rint(q).astype(np.int8))
+
+
+def run_norm(torch, Q, x, delta, gain, d, eps=1e-6, x_out=None, ldq=None, stream=None):
+    M, ldq = x.shape[0], ldq or up(d, 128)
+    codes = torch.full((M, ldq), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((M,), -1.0, device="cuda")
+    Q.check(Q.dit_op_rmsnorm_i8(stream, x.data_ptr(), x.stride(0), None if delta is None else delta.data_ptr(),
+                                int(delta is not None and delta.dtype == torch.float32), 0 if delta is None else delta.stride(0), gain.data_ptr(), eps,
+                                M, d, None if x_out is None else x_out.data_ptr(), 0 if x_out is None else x_out.stride(0), codes.data_ptr(), ldq,
+                                scale.data_ptr()))
+    torch.cuda.synchronize()
+    return codes.cpu().numpy(), scale.cpu().numpy()
+
+
+def check_norm(codes, scale, xs, gain, d, eps=1e-6):
+    y = xs / np.sqrt((xs * xs).mean(axis=1, keepdims=True) + eps) * gain
+    s, _ = codes_of(y)
+    # the 64-bit norm may be on the other side of a border of two float32 numbers: a step of the scale is 2^-23 of it
+    assert (np.abs(scale.astype(np.float64) - s) <= 2.0 ** -23 * s).all()
+    assert (np.abs(y / scale[:, None].astype(np.float64) - codes[:, :d]) <= 0.5 + 1e-9).all()
+    assert not codes[:, d:up(d, 128)].any() and (codes[:, up(d, 128):] == 77).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("delta", ["none", "bf16", "f32"])
+@pytest.mark.parametrize("out", ["none", "other", "same"])
+@pytest.mark.parametrize("M,d", [(1, 1), (5, 6), (3, 256), (9, 300), (4, 1024), (2, 1536), (3, 2047), (7, 4096), (33, 4097), (2, 5120), (3, 8192), (2, 16381)])
+def test_norm_with_codes(torch, Q, delta, out, M, d):
+    g = torch.Generator().manual_seed(M * 31 + d)
+    ldx = up(d, 8) + 8
+    x = torch.randn(M, ldx, generator=g) * torch.exp(2 * torch.randn(M, 1, generator=g))
+    x[:, d // 3] *= 30.0
+    if M > 2:
+        x[1] = 0.0
+    gain = (1 + 0.3 * torch.randn(d, generator=g)).cuda()
+    dl = None if delta == "none" else torch.randn(M, ldx, generator=g).to(torch.bfloat16 if delta == "bf16" else torch.float32)
+    if M > 2 and dl is not None:
+        dl[1] = 0.0                                                  # a row of zeros
+    want = x[:, :d] if dl is None else x[:, :d] + dl[:, :d].float()
+    xd, dd = x.cuda(), None if dl is None else dl.cuda()
+    xo = {"none": None, "same": xd, "other": torch.full((M, ldx + 4), 5.0, device="cuda")}[out]
+    codes, scale = run_norm(torch, Q, xd, dd, gain, d, x_out=xo, ldq=up(d, 128) + 16)
+    check_norm(codes, scale, want.double().numpy(), gain.double().cpu().numpy(), d)
+    if out == "none":
+        assert torch.equal(xd.cpu(), x)
+    else:
+        assert torch.equal(xo[:, :d].cpu(), want)
+        assert torch.equal(xo[:, d:].cpu(), x[:, d:] if out == "same" else torch.full((M, ldx + 4 - d), 5.0))
+
+
+@pytest.mark.gpu
+def test_norm_of_extreme_rows(torch, Q):
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(9, 640, generator=g).cuda()
+    gain = torch.ones(640, device="cuda")
+    x[0, 3], x[1, 639], x[2, 100] = math.inf, math.nan, -math.inf
+    x[3] *= 1e-30                                                    # far below eps
+    x[4] *= 1e37                                                     # squares past float32
+    x[5] = 3e38
+    codes, scale = run_norm(torch, Q, x, None, gain, 640, ldq=656)
+    assert np.isnan(scale[:3]).all() and not codes[:3, :640].any()
+    check_norm(codes[3:], scale[3:], x[3:].double().cpu().numpy(), np.ones(640), 640)
+    # an overflow in the sum is an infinity of its row alone
+    y = x.clone()
+    codes, scale = run_norm(torch, Q, y, torch.full_like(y, 2e38), gain, 640, x_out=y, ldq=656)
+    assert np.isnan(scale[[0, 1, 2, 5]]).all() and np.isfinite(scale[[3, 4, 6, 7, 8]]).all() and torch.isinf(y[5]).all()
+    # a gain that is no number spoils every row, one of zero none
+    gain[7] = math.nan
+    assert np.isnan(run_norm(torch, Q, x, None, gain, 640, ldq=656)[1]).all()
+    gain[7] = 0.0
+    codes, scale = run_norm(torch, Q, x, None, gain, 640, ldq=656)
+    assert not codes[:, 7].any() and np.isfinite(scale[3:]).all()
+
+
+# ------------------------------------------------------------------------------------------------ products
+class Product:
+    """Operands of one product: codes with strides of their own and unrelated codes between the rows."""
+
+    def __init__(self, torch, M, N, K, seed=1, pad_a=0, pad_w=0, pair=False):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.torch, self.M, self.N, self.K = torch, M, N, K
+        code = lambda r, ld: torch.randint(-128, 128, (r, ld), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)  # noqa: E731
+        self.A, self.W = code(M, K + pad_a), code(N, K + pad_w)
+        self.sa = 0.01 * (0.5 + torch.rand(M, generator=g, device="cuda"))
+        self.sw = (0.5 + torch.rand(N, generator=g, device="cuda")) / (50.0 * math.sqrt(K))
+        self.bias = torch.randn(N, generator=g, device="cuda")
+        self.work = torch.full((8 << 20,), -1, dtype=torch.int32, device="cuda")
+        if pair:
+            self.W2, self.sw2 = code(N, K + pad_w), (0.5 + torch.rand(N, generator=g, device="cuda")) / (50.0 * math.sqrt(K))
+
+    def exact(self, W=None, sw=None):
+        """(product without the bias in 64 bits)"""
+        W, sw = self.W if W is None else W, self.sw if sw is None else sw
+        p = self.A[:, :self.K].double() @ W[:, :self.K].double().t().contiguous()
+        return p * self.sa.double()[:, None] * sw.double()
+
+    def plain(self, Q, kind, bias=True, out=None, gate=None, row_req=None, rows=slice(None), work=True, stream=None):
+        torch = self.torch
+        A, sa = self.A[rows], self.sa[rows]
+        f32 = kind in (1, 3)
+        ldc = up(self.N, 8) + 8
+        if out is None:
+            out = torch.full((A.shape[0], ldc), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        Q.check(Q.dit_op_gemm_i8(stream, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.W.stride(0), self.sw.data_ptr(),
+                                 self.bias.data_ptr() if bias else None, A.shape[0], self.N, self.K, kind, out.data_ptr(), ldc,
+                                 None if gate is None else gate.data_ptr(), 0 if gate is None else gate.stride(0),
+                                 None if row_req is None else row_req.data_ptr(), self.work.data_ptr() if work else None,
+                                 self.work.numel() * 4 if work else 0))
+        return out
+
+    def pair(self, Q, rows=slice(None), work=True):
+        torch = self.torch
+        A, sa = self.A[rows], self.sa[rows]
+        ldc = up(self.N, 8) + 8
+        out = torch.full((A.shape[0], ldc), 9.0, dtype=torch.bfloat16, device="cuda")
+        Q.check(Q.dit_op_gemm_i8_geglu(None, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.sw.data_ptr(), self.W2.data_ptr(),
+                                       self.sw2.data_ptr(), self.W.stride(0), A.shape[0], self.N, self.K, out.data_ptr(), ldc,
+                                       self.work.data_ptr() if work else None, self.work.numel() * 4 if work else 0))
+        return out
+
+    def transposed(self, Q, col, ldo, bias=True, rows=slice(None), work=True):
+        torch = self.torch
+        A, sa = self.A[rows], self.sa[rows]
+        out = torch.full((self.N, ldo), 9.0, dtype=torch.bfloat16, device="cuda")
+        Q.check(Q.dit_op_gemm_i8_transposed(None, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.W.stride(0), self.sw.data_ptr(),
+                                            self.bias.data_ptr() if bias else None, A.shape[0], self.N, self.K, out.data_ptr(), ldo, col.data_ptr(),
+                                            self.work.data_ptr() if work else None, self.work.numel() * 4 if work else 0))
+        return out
+
+
+def gelu64(v):
+    t = math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)
+    return v * (2 * t).sigmoid()
+
+
+# The float arithmetic of one result: the sum to float32, the factor of two scales, the fused product and sum: three roundings.
+def product_bound(p, b):
+    return 3.01 * F32 * (p.abs() + abs(b))
+
+
+# GELU: its argument's exponent is off by a few roundings of a number up to 2.9 t, and a result for large negative arguments vanishes;
+# exponential and reciprocal are off by 2^-22 each.
+def gelu_bound(v, dv):
+    t = (math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)).abs().clamp(max=64.0)
+    return gelu64(v).abs() * (8 * F32 * (1 + 3 * t) + 2 * 2.0 ** -22) + 1.13 * dv + 1e-30
+
+
+SHAPES = [(1, 1, 128), (1, 256, 128), (2, 17, 256), (1, 4096, 4096), (7, 100, 1280), (16, 512, 384), (17, 520, 2048), (31, 64, 10240), (32, 1536, 1536), (33, 1000, 512),
+          (48, 768, 4096), (63, 130, 640), (64, 4096, 512), (65, 333, 1152), (77, 2048, 4096), (96, 250, 256), (127, 384, 10240), (128, 1280, 1280), (129, 1536, 128),
+          (200, 4096, 1024), (255, 257, 768), (256, 256, 4096), (300, 5120, 256), (333, 1000, 1536), (500, 4096, 2560), (640, 640, 384), (1000, 1537, 512), (1137, 4096, 256),
+          (2049, 1100, 256), (4100, 2304, 128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product_of_codes_in_every_form(torch, Q, M, N, K):
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=48, pad_w=16)
+    p, b = P.exact(), P.bias.double()
+    for work in (True, False):
+        for bias in (True, False):
+            v = p + b if bias else p
+            dv = product_bound(p, b if bias else 0.0 * b)
+            for kind in (0, 1, 2):
+                out = P.plain(Q, kind, bias, work=work)
+                want, tol = (gelu64(v), gelu_bound(v, dv)) if kind == 2 else (v, dv)
+                if kind != 1:
+                    tol = tol + BF16 * (want.abs() + tol)
+                d = (out[:, :N].double() - want).abs()
+                assert bool((d <= tol).all()), (kind, bias, work, float((d - tol).max()))
+                assert bool((out[:, N:] == 9.0).all())
+        # into the residual: every row's own gate, one gate, none
+        x = torch.randn(M, up(N, 8) + 8, generator=torch.Generator().manual_seed(2)).cuda()
+        gate = torch.randn(3, N + 1, generator=torch.Generator().manual_seed(3)).cuda()
+        req = (torch.arange(M) * 3 // M).to(torch.int32).cuda()
+        for gt, rr in ((gate, req), (gate, None), (None, None)):
+            out = P.plain(Q, 3, out=x.clone(), gate=gt, row_req=rr, work=work)
+            gv = 1.0 if gt is None else gate[0, :N].double() if rr is None else gate.double()[req.long()][:, :N]
+            want = x[:, :N].double() + gv * (p + b)
+            tol = 1.01 * F32 * want.abs() + abs(gv) * product_bound(p, b) if gt is not None else 1.01 * F32 * want.abs() + product_bound(p, b)
+            d = (out[:, :N].double() - want).abs()
+            assert bool((d <= tol).all()), (work, float((d - tol).max()))
+            assert torch.equal(out[:, N:], x[:, N:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gated_pair_of_codes(torch, Q, M, N, K):
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=16, pad_w=32, pair=True)
+    g, u = P.exact(), P.exact(P.W2, P.sw2)
+    zero = 0.0 * P.bias.double()
+    dg, du = gelu_bound(g, product_bound(g, zero)), product_bound(u, zero)
+    want = gelu64(g) * u
+    tol = dg * u.abs() + gelu64(g).abs() * du + dg * du
+    tol = tol + (BF16 + F32) * (want.abs() + tol)
+    for work in (True, False):
+        out = P.pair(Q, work=work)
+        d = (out[:, :N].double() - want).abs()
+        assert bool((d <= tol).all()), (work, float((d - tol).max()))
+        assert bool((out[:, N:] == 9.0).all())
+
+
+def columns(M, kind):
+    """Columns that rise: all neighbours from an even or odd start on, ragged prompts at multiples of 64, or every other one."""
+    if kind == "packed":
+        return np.arange(M) + 8
+    if kind == "odd":
+        return np.arange(M) + 5
+    if kind == "sparse":
+        return np.arange(M) * 2 + 1
+    col, at, k = [], 0, 0
+    while len(col) < M:
+        n = min((31, 200, 7, 64, 77, 1, 130)[k % 7], M - len(col))
+        col += range(at, at + n)
+        at += up(n, 64)
+        k += 1
+    return np.array(col)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["ragged", "packed", "odd", "sparse"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 128), (1, 300, 256), (17, 520, 2048), (32, 4096, 512), (64, 256, 4096), (77, 1030, 512), (130, 512, 640), (300, 768, 1280), (511, 4096, 256),
+                                   (1137, 2048, 256), (2049, 1100, 128)])
+def test_product_of_codes_transposed(torch, Q, kind, M, N, K):
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=16)
+    c = columns(M, kind)
+    ldo = up(int(c[-1]) + 1, 8) + 16
+    col = torch.from_numpy(c.astype(np.int32)).cuda()
+    for bias in (True, False):
+        v = P.exact() + (P.bias.double() if bias else 0.0)
+        dv = product_bound(P.exact(), P.bias.double() if bias else 0.0 * P.bias.double())
+        for work in (True, False):
+            out = P.transposed(Q, col, ldo, bias, work=work)
+            got = out[:, col.long()].t().double()
+            assert bool(((got - v).abs() <= dv + BF16 * (v.abs() + dv)).all())
+            rest = torch.ones(ldo, dtype=torch.bool, device="cuda")
+            rest[col.long()] = False
+            assert bool((out[:, rest] == 9.0).all())
+
+
+@pytest.mark.gpu
+def test_a_row_is_the_same_whatever_its_neighbours(torch, Q):
+    """One product of 2100 rows and parts of it, which take other tiles and other shares of K: not a bit differs."""
+    P = Product(torch, 2100, 1536, 1536, pair=True)
+    col = torch.arange(2100, dtype=torch.int32, device="cuda")
+    full = {k: P.plain(Q, k) for k in (0, 1, 2)}
+    pair, tr = P.pair(Q), P.transposed(Q, col, 2104)
+    for a, n in ((0, 1), (5, 16), (40, 33), (100, 64), (200, 77), (300, 129), (512, 256), (700, 500), (1000, 1100)):
+        rows = slice(a, a + n)
+        for work in (True, False):
+            for k in (0, 1, 2):
+                assert torch.equal(P.plain(Q, k, rows=rows, work=work), full[k][rows])
+            assert torch.equal(P.pair(Q, rows=rows, work=work), pair[rows])
+            assert torch.equal(P.transposed(Q, col, up(n, 8), rows=rows, work=work)[:, :n], tr[:, rows])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_longest_sum_stays_exact(torch, Q, M):
+    """Every code -128 at the largest K: the sum is 2^14 K, just inside 32 bits; and one of both signs that cancels."""
+    K = Q.MAX_K
+    P = Product(torch, M, 20, K)
+    P.A.fill_(-128)
+    P.W.fill_(-128)
+    P.W[1, ::2] = 127
+    P.sa.fill_(1.0)
+    P.sw.fill_(1.0)
+    out = P.plain(Q, 1, bias=False)
+    assert bool((out[:, 0] == 16384.0 * K).all()) and bool((out[:, 1] == float(np.float32(128 * 128 * (K // 2) - 128 * 127 * (K // 2)))).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 70, 400])
+def test_infinities_and_nan_stay_in_their_rows_and_columns(torch, Q, M):
+    P = Product(torch, M, 300, 256)
+    clean = P.plain(Q, 1, bias=False)
+    P.sa[1], P.sw[7], P.sw[250] = math.nan, math.inf, math.nan
+    out = P.plain(Q, 1, bias=False)
+    keep = torch.ones(300, dtype=torch.bool, device="cuda")
+    keep[[7, 250]] = False
+    rows = torch.ones(M, dtype=torch.bool, device="cuda")
+    rows[1] = False
+    assert bool(torch.isnan(out[1, :300]).all()) and bool(torch.isnan(out[:, 250]).all()) and not bool(torch.isfinite(out[:, 7]).any())
+    assert torch.equal(out[rows][:, :300][:, keep], clean[rows][:, :300][:, keep])
+    assert bool(torch.isnan(P.plain(Q, 0)[1, :300].float()).all()) and bool(torch.isnan(P.plain(Q, 2)[1, :300].float()).all())
+
+
+# ------------------------------------------------------------------------------------------------ together
+class Mlp:
+    """Norm, gated pair, quantiser and output product in a row, as the encoder runs them."""
+
+    def __init__(self, torch, M, d=512, ff=1280, seed=1):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+        self.torch, self.M, self.d, self.ff = torch, M, d, ff
+        self.x0, self.delta, self.gain = rnd(M, d), rnd(M, d).bfloat16(), 1 + 0.1 * rnd(d)
+        self.w = [rnd(ff, d) / math.sqrt(d), rnd(ff, d) / math.sqrt(d), rnd(d, ff) / math.sqrt(ff)]
+        e = lambda *s, t=torch.int8: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+        f = torch.float32
+        self.wq, self.ws = [e(*w.shape) for w in self.w], [e(w.shape[0], t=f) for w in self.w]
+        self.h, self.hs, self.act, self.q, self.qs = e(M, d), e(M, t=f), e(M, ff, t=torch.bfloat16), e(M, ff), e(M, t=f)
+        self.x, self.out = e(M, d, t=f), e(M, d, t=f)
+        self.work = e(1 << 25)
+
+    def weights(self, Q, st=None):
+        for w, q, s in zip(self.w, self.wq, self.ws):
+            Q.check(Q.dit_op_quantize_i8(st, w.data_ptr(), 1, w.shape[1], w.shape[0], w.shape[1], q.data_ptr(), q.shape[1], s.data_ptr()))
+
+    def run(self, Q, st=None):
+        M, d, ff, n = self.M, self.d, self.ff, self.work.numel()
+        Q.check(Q.dit_op_rmsnorm_i8(st, self.x0.data_ptr(), d, self.delta.data_ptr(), 0, d, self.gain.data_ptr(), 1e-6, M, d, self.x.data_ptr(), d,
+                                    self.h.data_ptr(), d, self.hs.data_ptr()))
+        Q.check(Q.dit_op_gemm_i8_geglu(st, self.h.data_ptr(), d, self.hs.data_ptr(), self.wq[0].data_ptr(), self.ws[0].data_ptr(), self.wq[1].data_ptr(),
+                                       self.ws[1].data_ptr(), d, M, ff, d, self.act.data_ptr(), ff, self.work.data_ptr(), n))
+        Q.check(Q.dit_op_quantize_i8(st, self.act.data_ptr(), 0, ff, M, ff, self.q.data_ptr(), ff, self.qs.data_ptr()))
+        Q.check(Q.dit_op_gemm_i8(st, self.q.data_ptr(), ff, self.qs.data_ptr(), self.wq[2].data_ptr(), ff, self.ws[2].data_ptr(), None, M, d, ff, 3,
+                                 self.x.data_ptr(), d, None, 0, None, self.work.data_ptr(), n))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 30, 500, 1100])
+def test_chain_is_near_the_unquantised_one(torch, Q, M):
+    """Every code is off by at most half a step, independent of the others: a step is the row's largest magnitude / 127, about 4
+    sigma of a gaussian row, so an operand's relative error is 4 / 127 / sqrt(12) = 0.9 % (rms).  Two operands of each of the
+    two input products give sqrt(4) of it, the gated activation with its heavier tails two of it, the output weights one: together
+    2.7 %, and the slope of GELU makes the gate's part up to twice as large: below 4 %."""
+    m = Mlp(torch, M)
+    m.weights(Q)
+    m.run(Q)
+    torch.cuda.synchronize()
+    x = (m.x0 + m.delta.float()).double()
+    h = x / (x.square().mean(1, keepdim=True) + 1e-6).sqrt() * m.gain.double()
+    a = gelu64(h @ m.w[0].double().t().contiguous()) * (h @ m.w[1].double().t().contiguous())
+    branch = a @ m.w[2].double().t().contiguous()
+    off = (m.x.double() - x - branch).norm() / branch.norm()
+    assert float(off) <= 0.04, float(off)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 70, 600])
+def test_chain_on_a_stream_and_in_a_graph(torch, Q, M):
+    """The chain on a stream of its own, captured and replayed several times with other inputs and eager work between the
+    replays: every replay leaves what an eager run leaves, bit for bit."""
+    m = Mlp(torch, M)
+    m.weights(Q)
+    m.run(Q)
+    torch.cuda.synchronize()
+    want = m.x.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    m.x.zero_()
+    with torch.cuda.stream(side):
+        m.run(Q, side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(m.x, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.run(Q, torch.cuda.current_stream().cuda_stream)
+    first = m.x0.clone()
+    for k in range(4):
+        m.x0.copy_(first * (1.0 + 0.25 * k))
+        m.work.fill_(-1)
+        m.run(Q)
+        torch.cuda.synchronize()
+        want = m.x.clone()
+        m.x.zero_(), m.act.zero_(), m.q.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m.x, want)
+
+
+@pytest.mark.gpu
+def test_two_streams_with_scratch_of_their_own(torch, Q):
+    """Two chains at the same time, each with its own buffers."""
+    a, b = Mlp(torch, 333, seed=1), Mlp(torch, 64, seed=2)
+    want = []
+    for m in (a, b):
+        m.weights(Q)
+        m.run(Q)
+        torch.cuda.synchronize()
+        want.append(m.x.clone())
+        m.x.zero_()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.run(Q, sa.cuda_stream)
+        b.run(Q, sb.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a.x, want[0]) and torch.equal(b.x, want[1])
