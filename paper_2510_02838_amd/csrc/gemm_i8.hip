@@ -3,20 +3,27 @@
 // The sum is held in 32-bit integers, exact for K < 2^17, so no way of cutting the product up changes a bit of the result; the
 // epilogue's float arithmetic is written with explicit fused operations, the same in every kernel.
 #include "int8_internal.h"
+#include <type_traits>
 
 namespace dit {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* lptr_t;
+typedef const __attribute__((address_space(4))) GemmI8 Problem;
 
 namespace {
 
-__device__ __forceinline__ uint16_t bf(float f) {
-  uint32_t u = __float_as_uint(f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0;    // (rounding would carry some NaN over to -0)
-  u += 0x7FFFu + ((u >> 16) & 1u);
-  return (uint16_t)(u >> 16);
+// round to nearest even (v_cvt_pk_bf16_f32)
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const f32x2 v = {a, b};
+  const bf16x2 r = __builtin_convertvector(v, bf16x2);
+  return *(const uint32_t*)&r;
 }
+__device__ __forceinline__ bf16_t bf(float f) { return (bf16_t)pack2(f, 0.f); }
 // 0.5 x (1 + tanh(u)) = x / (1 + 2^(-2 log2(e) u)), u = sqrt(2/pi) (x + 0.044715 x^3)
 __device__ __forceinline__ float gelu(float x) {
   const float t = x * __builtin_fmaf(0.035677408136300125f * x, x, 0.7978845608028654f);
@@ -25,67 +32,936 @@ __device__ __forceinline__ float gelu(float x) {
 }
 __device__ __forceinline__ float value(int acc, float sa, float sw, float bias) { return __builtin_fmaf((float)acc, sa * sw, bias); }
 
-// one result to its place
-__device__ __forceinline__ void put(const GemmI8& P, int m, int n, int acc) {
-  if (m >= P.M || n >= P.N) return;
-  float v = value(acc, P.sa[m], P.sw[n], P.bias ? P.bias[n] : 0.f);
-  if (n >= P.vt_from) { P.vt[(size_t)(n - P.vt_from) * P.ldvt + P.vt_col[m]] = bf(v); return; }
-  const size_t o = (size_t)m * P.ldc + n;
-  if (P.kind == OUT_F32) ((float*)P.out)[o] = v;
-  else if (P.kind == OUT_RESID_F32) {
-    const float g = P.gate ? P.gate[(size_t)(P.row_req ? P.row_req[m] : 0) * P.gate_stride + n] : 1.f;
-    ((float*)P.out)[o] = __builtin_fmaf(g, v, ((float*)P.out)[o]);
-  } else ((bf16_t*)P.out)[o] = bf(P.kind == OUT_GELU_BF16 ? gelu(v) : v);
+// Four neighbouring columns of a row to their places (n + 3 may be past the end); up: the same columns of a pair's second product.
+template <class P>
+__device__ __forceinline__ void put_row4(const P& p, int m, int n, const i32x4& acc) {
+  const float sa = p.sa[m];
+  const int left = p.N - n < 4 ? p.N - n : 4;
+  float v[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int k = c < left ? n + c : n;
+    v[c] = value(acc[c], sa, p.sw[k], p.bias ? p.bias[k] : 0.f);
+  }
+  if (n >= p.vt_from) {
+    const int col = p.vt_col[m];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c < left) p.vt[(size_t)(n + c - p.vt_from) * p.ldvt + col] = bf(v[c]);
+    return;
+  }
+  const size_t o = (size_t)m * p.ldc + n;
+  if (p.kind == OUT_F32 || p.kind == OUT_RESID_F32) {
+    float* out = (float*)p.out + o;
+    if (p.kind == OUT_RESID_F32) {
+      const float* g = p.gate ? p.gate + (size_t)(p.row_req ? p.row_req[m] : 0) * p.gate_stride + n : nullptr;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      if (left == 4) x = *(const f32x4*)out;
+      else
+        for (int c = 0; c < left; ++c) x[c] = out[c];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(g ? g[c < left ? c : 0] : 1.f, v[c], x[c]);
+    }
+    if (left == 4) *(f32x4*)out = f32x4{v[0], v[1], v[2], v[3]};
+    else
+      for (int c = 0; c < left; ++c) out[c] = v[c];
+  } else {
+    bf16_t* out = (bf16_t*)p.out + o;
+    if (p.kind == OUT_GELU_BF16) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = gelu(v[c]);
+    }
+    if (left == 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    else
+      for (int c = 0; c < left; ++c) out[c] = bf(v[c]);
+  }
 }
-__device__ __forceinline__ void put_pair(const GemmI8& P, int m, int n, int gate, int up) {
-  if (m >= P.M || n >= P.N) return;
-  const float sa = P.sa[m];
-  ((bf16_t*)P.out)[(size_t)m * P.ldc + n] = bf(gelu(value(gate, sa, P.sw[n], 0.f)) * value(up, sa, P.sw2[n], 0.f));
+template <class P>
+__device__ __forceinline__ void put_pair4(const P& p, int m, int n, const i32x4& gate, const i32x4& up) {
+  const float sa = p.sa[m];
+  const int left = p.N - n < 4 ? p.N - n : 4;
+  float v[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int k = c < left ? n + c : n;
+    v[c] = gelu(value(gate[c], sa, p.sw[k], 0.f)) * value(up[c], sa, p.sw2[k], 0.f);
+  }
+  bf16_t* out = (bf16_t*)p.out + (size_t)m * p.ldc + n;
+  if (left == 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+  else
+    for (int c = 0; c < left; ++c) out[c] = bf(v[c]);
+}
+// four neighbouring rows of a column of the transposed part (m + 3 may be past the end)
+template <class P>
+__device__ __forceinline__ void put_col4(const P& p, int m, int n, const i32x4& acc) {
+  const float sw = p.sw[n], b = p.bias ? p.bias[n] : 0.f;
+  bf16_t* dst = p.vt + (size_t)(n - p.vt_from) * p.ldvt;
+  int col[4];
+  bf16_t v[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int k = m + c < p.M ? m + c : m;
+    col[c] = p.vt_col[k];
+    v[c] = bf(value(acc[c], p.sa[k], sw, b));
+  }
+  if (m + 4 <= p.M && col[3] == col[0] + 3 && (col[0] & 3) == 0)       // (columns rise)
+    *(uint2*)(dst + col[0]) = make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
+  else {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (m + c < p.M) dst[col[c]] = v[c];
+  }
+}
+
+// at most N vector-memory loads outstanding; LGKM0: LDS reads done too
+template <int N, bool LGKM0>
+__device__ __forceinline__ void wait_vm() {
+  constexpr int imm = (N & 15) | ((N >> 4) << 14) | (7 << 4) | ((LGKM0 ? 0 : 15) << 8);
+  __builtin_amdgcn_s_waitcnt(imm);
+  asm volatile("" ::: "memory");
+}
+// barrier without the fence of __syncthreads(), which would wait for every load in flight
+__device__ __forceinline__ void wg_barrier() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void buffer_load_lds16(const void* base, lptr_t dst, uint32_t voff, int soff) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)0xFFFFFFFFu, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, soff, 0, 0);
+}
+// key of a slab row: 16 rows fall into 16 distinct 16-byte slots, consecutive ones and those of the permuted order below
+__device__ __forceinline__ int swz_key(int r) { return ((r >> 1) & 1) | ((r >> 2) & 2) | ((r ^ (r >> 2)) & 4); }
+
+// tile t -> (tile row, tile column): groups of 8 tile rows, column-major inside
+template <class P>
+__device__ __forceinline__ void tile_coords(const P& p, int t, int& tm, int& tn) {
+  const int per = 8 * p.tiles_n, g = t / per, r = t - g * per, first = g * 8;
+  const int gsz = p.tiles_m - first < 8 ? p.tiles_m - first : 8;
+  tm = first + r % gsz;
+  tn = r / gsz;
 }
 
 }  // namespace
 
-// 64x64 tile, 4 waves of 32x32, operand fragments straight from memory: lane l holds 16 codes of row l % 16 from k = 16 (l / 16) on.
-template <bool PAIR>
-__global__ __launch_bounds__(256) void gemm_i8_simple_kernel(const GemmI8 P) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, kq = lane >> 4;
-  const int m0 = blockIdx.y * 64 + (wave >> 1) * 32, n0 = blockIdx.x * 64 + (wave & 1) * 32;
-  i32x4 acc[2][2] = {}, acc2[2][2] = {};
-  const int8_t *a[2], *b[2], *b2[2];
-  for (int i = 0; i < 2; ++i) {
-    const int m = m0 + i * 16 + l16, n = n0 + i * 16 + l16;     // rows past the end repeat the last one and are not stored
-    a[i] = P.A + (size_t)(m < P.M ? m : P.M - 1) * P.lda + kq * 16;
-    b[i] = P.W + (size_t)(n < P.N ? n : P.N - 1) * P.ldw + kq * 16;
-    b2[i] = PAIR ? P.W2 + (size_t)(n < P.N ? n : P.N - 1) * P.ldw + kq * 16 : b[i];
+// ---- 8-wave tiles ----------------------------------------------------------------------------------------------------
+//
+// A workgroup of two groups of four waves (one wave of each on every SIMD), half a phase apart: while one group does nothing
+// but multiply, the other reads its next fragments from LDS and issues the loads of later slabs.  Slabs are 128 codes wide and
+// go from memory straight into an NS-stage LDS ring; a workgroup stays on its CU and the slabs of its tiles (or of its shares of
+// K) are one stream, so the next tile's first slabs arrive under the epilogue.
+// Operands are swapped (W in the place of the MFMA's rows, its rows in the order {0-3, 8-11, ...}, {4-7, ...}), which gives a lane
+// 8 neighbouring columns of one row; tiles of transposed results keep the first order with the rows of A permuted.
+template <int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
+  Problem& P = *(Problem*)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int ROWB = 128;
+  constexpr int RT = BM / WM / 16, CT = 4;             // 16-row and 16-column tiles of a wave
+  constexpr int PH = NS == 2 ? 2 : 1, RP = RT / PH;    // phases per slab, row tiles per phase
+  constexpr int LA = BM / 64, LB = BN / 64, LPS = LA + LB;   // loads per wave and slab
+  constexpr int LAU = NS == 2 ? WM : LA;               // ... of the first part of A: 64 rows of every wave row
+  constexpr int STAGE = (BM + BN) * ROWB, OFFB = BM * ROWB;
+  static_assert(WM * WN == 8 && BN / WN == 64 && BM % 64 == 0 && RT % PH == 0, "two groups of four waves, 64 columns a wave");
+  static_assert(NS >= 3 || (NS == 2 && RP * 16 == 64), "two stages: 64 rows a phase");
+  static_assert((NS - 1) * LPS < 64, "vmcnt");
+  extern __shared__ __attribute__((aligned(128))) unsigned char smem[];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  unsigned char* const patch = smem + NS * STAGE + wave * 2048;
+  const int splits = P.splits;
+  const bool pair = P.W2 != nullptr;
+
+  // my units (a tile, or one share of K of a tile): XCD x (workgroup ids are dealt round-robin) owns a contiguous range of them
+  int t_first, t_count, t_step;
+  {
+    const int x = blockIdx.x & 7, T = P.tiles_m * P.tiles_n * splits, G = gridDim.x;
+    t_first = x * (T >> 3) + (x < (T & 7) ? x : (T & 7));
+    t_count = (T >> 3) + (x < (T & 7) ? 1 : 0);
+    t_step = (G >> 3) + (x < (G & 7) ? 1 : 0);
   }
-  for (int k = 0; k < P.K; k += 64) {
-    i32x4 fa[2], fb[2], fc[2];
-    for (int i = 0; i < 2; ++i) {
-      fa[i] = *(const i32x4*)(a[i] + k);
-      fb[i] = *(const i32x4*)(b[i] + k);
-      if (PAIR) fc[i] = *(const i32x4*)(b2[i] + k);
+  auto unit = [&](int t, int& tm, int& tn, int& k0, int& k1) {
+    const int u = t_first + t, tile = u / splits, sh = u - tile * splits, nk = P.K / 128;
+    tile_coords(P, tile, tm, tn);
+    k0 = (int)((long long)sh * nk / splits); k1 = (int)((long long)(sh + 1) * nk / splits);
+  };
+
+  // ---- the stream of slabs: one load of a wave fills 8 slab rows -------------------------------------------------------
+  auto row_a = [&](int i) {
+    if constexpr (NS == 2) {         // A in two parts, the first 64 rows of every wave row and the rest
+      const bool up = i < LAU;
+      const int per = up ? 64 : RT * 16 - 64;
+      const int rr = ((up ? i : i - LAU) * 8 + wave) * 8;
+      return rr / per * (RT * 16) + rr % per + (up ? 0 : 64);
+    } else {
+      return (i * 8 + wave) * 8;
     }
-    for (int i = 0; i < 2; ++i)
-      for (int j = 0; j < 2; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        if (PAIR) acc2[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fc[j], acc2[i][j], 0, 0, 0);
+  };
+  uint32_t oa[LA], ob[LB];           // byte offsets of my lane's 16 codes of each load, from the tile's first row
+  const int8_t *sA, *sW;
+  int ld_t = blockIdx.x >> 3, ks = 0, ks_n = 0;
+  auto aim = [&](int t) {
+    int tm, tn;
+    unit(t, tm, tn, ks, ks_n);
+    const int m0 = tm * BM, n0 = pair ? tn * (BN / 2) : tn * BN;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));     // (made anew for each tile: kept, these would cost registers)
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+      const int r = row_a(i) + (ln >> 3), c = (ln & 7) ^ swz_key(r);
+      const int m = m0 + r < P.M ? r : P.M - 1 - m0;             // clamp: rows past M are never stored
+      oa[i] = (uint32_t)m * (uint32_t)P.lda + c * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+      const int r = (i * 8 + wave) * 8 + (ln >> 3), c = (ln & 7) ^ swz_key(r);
+      const int rw = pair ? (r >> 6) * 32 + (r & 31) : r;
+      const int n = n0 + rw < P.N ? rw : P.N - 1 - n0;
+      ob[i] = (uint32_t)n * (uint32_t)P.ldw + c * 16;
+    }
+    sA = P.A + (size_t)m0 * P.lda;
+    sW = (pair && (wave & 4) ? P.W2 : P.W) + (size_t)n0 * P.ldw;    // (waves 4-7 load the upper half of each 64 rows)
+  };
+  // (behind the very last slab the same again, which keeps the number of loads per slab fixed)
+  auto advance = [&]() {
+    if (ks + 1 < ks_n) ++ks;
+    else if (ld_t + t_step < t_count) {
+      ld_t += t_step;
+      aim(ld_t);
+    }
+  };
+  auto issue_a = [&](int st, auto first, auto last) {
+#pragma unroll
+    for (int i = decltype(first)::value; i < decltype(last)::value; ++i)
+      buffer_load_lds16(sA, (lptr_t)(smem + st * STAGE + row_a(i) * ROWB), oa[i], ks * 128);
+  };
+  auto issue_b = [&](int st) {
+#pragma unroll
+    for (int i = 0; i < LB; ++i) buffer_load_lds16(sW, (lptr_t)(smem + st * STAGE + OFFB + (i * 8 + wave) * 1024), ob[i], ks * 128);
+  };
+  constexpr std::integral_constant<int, 0> A_FIRST{};
+  constexpr std::integral_constant<int, LAU> A_REST{};
+  constexpr std::integral_constant<int, LA> A_END{};
+
+  // ---- the loop over one unit's slabs --------------------------------------------------------------------------------
+  i32x4 acc[RT][CT];
+  const bool second = wave >= 4;
+  int stage = 0;
+  auto run = [&](auto vt_tag, int nk) {
+    constexpr bool VT = decltype(vt_tag)::value;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int l16 = ln & 15, kq = ln >> 4;
+    const int row_c = l16, row_p = (l16 >> 2) * 8 + (l16 & 3);
+    const int off_c = row_c * ROWB + ((kq ^ swz_key(row_c)) << 4), off_p = row_p * ROWB + ((kq ^ swz_key(row_p)) << 4);
+    i32x4 fa[2][RP], fb[2][CT];
+    // consecutive rows: 16-row tile i starts 16 i rows on; permuted ones: pairs of tiles 32 rows on, the odd one 4 rows on
+    auto tile_off = [](bool perm, int i) { return perm ? (i >> 1) * 32 + (i & 1) * 4 : i * 16; };
+    const int a0 = wm * (RT * 16) * ROWB + (VT ? off_p : off_c), b0 = OFFB + wn * 64 * ROWB + (VT ? off_c : off_p);
+    auto read_a = [&](const unsigned char* st, auto phase) {
+      const unsigned char* p[2] = {st + a0, st + (a0 ^ 64)};     // (odd tiles flip bit 2 of the key)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int r = 0; r < RP; ++r) {
+          const int i = decltype(phase)::value * RP + r;
+          fa[k][r] = *(const i32x4*)(p[k ^ (i & 1)] + tile_off(VT, i) * ROWB);
+        }
+    };
+    auto read_b = [&](const unsigned char* st) {
+      const unsigned char* p[2] = {st + b0, st + (b0 ^ 64)};
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) fb[k][c] = *(const i32x4*)(p[k ^ (c & 1)] + tile_off(!VT, c) * ROWB);
+    };
+    auto multiply = [&](auto phase) {
+      wg_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int r = 0; r < RP; ++r)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            i32x4& d = acc[decltype(phase)::value * RP + r][c];
+            if constexpr (VT) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[k][r], fb[k][c], d, 0, 0, 0);
+            else d = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[k][c], fa[k][r], d, 0, 0, 0);
+          }
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      wg_barrier();
+    };
+    constexpr std::integral_constant<int, 0> P0{};
+    constexpr std::integral_constant<int, PH - 1> P1{};
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) acc[r][c] = i32x4{0, 0, 0, 0};
+    auto slab = [&](auto same) {       // same: the stream's next slab is known to be of this unit
+      const unsigned char* cur = smem + stage * STAGE;
+      const int nxt = stage + 1 == NS ? 0 : stage + 1;
+      if constexpr (decltype(same)::value) ++ks; else advance();
+      read_b(cur);
+      read_a(cur, P0);
+      if constexpr (NS == 2) {
+        // Phase 0 of slab s reads the first part of A and W; phase 1 the rest of A, and issues W and the first part of A
+        // of slab s+2; when it is over the rest of A follows (over that of slab s, which everybody has read).
+        wait_vm<LPS, true>();                          // rest of A of slab s (mine)
+        multiply(P0);
+        read_a(cur, P1);
+        issue_b(stage); issue_a(stage, A_FIRST, A_REST);
+        wait_vm<LPS, true>();                          // W and the first part of A of slab s+1 (mine)
+        multiply(P1);
+        issue_a(stage, A_REST, A_END);
+      } else {
+        // phase s reads slab s and issues slab s + NS - 1 into the stage that slab s-1 left
+        const int free_st = stage == 0 ? NS - 1 : stage - 1;
+        issue_a(free_st, A_FIRST, A_END); issue_b(free_st);
+        wait_vm<(NS - 2) * LPS, true>();               // slab s+1 (mine)
+        multiply(P0);
       }
+      stage = nxt;
+    };
+    if (second) wg_barrier();
+    int kt = 0;
+    for (; kt < nk - (NS == 2 ? 2 : NS - 1); ++kt) slab(std::true_type{});
+    for (; kt < nk; ++kt) slab(std::false_type{});
+    if (!second) wg_barrier();
+  };
+
+  // ---- epilogues: C[16 r + l16][32 j + 8 kq + 0..7] of the wave's sub-tile in acc[r][2 j], acc[r][2 j + 1] ------------
+  auto epilogue = [&](int tm, int tn, bool vt) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int l16 = ln & 15, kq = ln >> 4;
+    const int prow = ln >> 3, pchunk = ln & 7;           // my row (and the one 8 on) and 16-byte chunk when a patch is read back
+    const int mw = tm * BM + wm * (RT * 16), nw = tn * BN + wn * 64;
+    const int M = P.M, N = P.N;
+    const float* const bias = P.bias;
+    auto patch_at = [&](int row, int chunk) { return patch + row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4); };
+    auto turn = [&](const u32x4& lo, const u32x4& hi, int c_lo, int c_hi, u32x4 (&out)[2]) {    // 16 rows x 128 bytes
+      *(u32x4*)patch_at(l16, c_lo) = lo;
+      *(u32x4*)patch_at(l16, c_hi) = hi;
+      asm volatile("" ::: "memory");                     // (a wave's LDS accesses are executed in order)
+      out[0] = *(const u32x4*)patch_at(prow, pchunk);
+      out[1] = *(const u32x4*)patch_at(prow + 8, pchunk);
+      asm volatile("" ::: "memory");
+    };
+    auto row_scale = [&](int m) { return P.sa[m < M ? m : M - 1]; };
+    auto load_cols = [&](const float* p, int n0, int n_end, float (&v)[8]) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] = p && n0 + c < n_end ? p[n0 + c] : 0.f;
+    };
+    float sa[RT];
+    auto load_sa = [&]() {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) sa[r] = row_scale(mw + r * 16 + l16);
+    };
+    auto plain_bf16 = [&](auto gelu_tag) {
+      float sw[2][8], bv[2][8];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { load_cols(P.sw, nw + j * 32 + kq * 8, N, sw[j]); load_cols(bias, nw + j * 32 + kq * 8, N, bv[j]); }
+      load_sa();
+      const bool full = nw + pchunk * 8 + 8 <= N;
+      const int ldc = P.ldc;
+      bf16_t* const out = (bf16_t*)P.out;
+      const uint32_t voff = (uint32_t)(prow * ldc + pchunk * 8) * 2u;
+      auto make = [&](int r, u32x4 (&w)[2]) {
+        u32x4 p[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float v[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            v[c] = value(acc[r][2 * j + (c >> 2)][c & 3], sa[r], sw[j][c], bv[j][c]);
+            if constexpr (decltype(gelu_tag)::value) v[c] = gelu(v[c]);
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) p[j][c] = pack2(v[2 * c], v[2 * c + 1]);
+        }
+        turn(p[0], p[1], kq, 4 + kq, w);
+      };
+      u32x4 w[2], nx[2];
+      make(0, w);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (r + 1 < RT) make(r + 1, nx);                 // (a unit is turned while the one before it is stored)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          char* const xp = (char*)(out + (size_t)(mw + r * 16 + h * 8) * ldc + nw) + voff;
+          if (prow < M - mw - (r * 16 + h * 8)) {
+            if (full) *(u32x4*)xp = w[h];
+            else
+              for (int c = 0; c < N - nw - pchunk * 8; ++c) ((bf16_t*)xp)[c] = (bf16_t)(w[h][c >> 1] >> (16 * (c & 1)));
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = nx[h];
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // fp32 results in units of 16 rows x 32 columns: plain, or added to what is there times the row's gate
+    auto plain_f32 = [&](auto resid_tag) {
+      constexpr bool RESID = decltype(resid_tag)::value;
+      float sw[2][8], bv[2][8];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { load_cols(P.sw, nw + j * 32 + kq * 8, N, sw[j]); load_cols(bias, nw + j * 32 + kq * 8, N, bv[j]); }
+      load_sa();
+      const int nb = nw + pchunk * 4, ldc = P.ldc;       // my columns on the way out: nb + 32 j ... + 3
+      float* const out = (float*)P.out;
+      const uint32_t voff = (uint32_t)(prow * ldc + pchunk * 4) * 4u;
+      auto row_at = [&](int u, int h) { return (char*)(out + (size_t)(mw + (u >> 1) * 16 + h * 8) * ldc + nw + 32 * (u & 1)) + voff; };
+      auto row_in = [&](int u, int h) { return prow < M - mw - (u >> 1) * 16 - h * 8; };
+      constexpr int U = RT * 2, AHEAD = 2;
+      f32x4 xr[RESID ? AHEAD : 1][2], gr[RESID ? AHEAD : 1][2];
+      const float* const gate = RESID ? P.gate : nullptr;
+      const int* const rreq = P.row_req;
+      // what is there, and the gate, AHEAD units before their use (the compiler may not move loads across the stores)
+      auto load_x = [&](int u) {
+        if constexpr (RESID) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f}, g = {1.f, 1.f, 1.f, 1.f};
+            const int n = nb + 32 * (u & 1);
+            if (row_in(u, h) && n < N) {
+              const float* xp = (const float*)row_at(u, h);
+              const float* gp = gate ? gate + (size_t)(rreq ? rreq[mw + (u >> 1) * 16 + h * 8 + prow] : 0) * P.gate_stride + n : nullptr;
+              if (n + 4 <= N) {
+                x = *(const f32x4*)xp;
+                if (gp) g = f32x4{gp[0], gp[1], gp[2], gp[3]};
+              } else {
+#pragma unroll
+                for (int c = 0; c < 3; ++c)
+                  if (n + c < N) {
+                    x[c] = xp[c];
+                    if (gp) g[c] = gp[c];
+                  }
+              }
+            }
+            xr[u % AHEAD][h] = x; gr[u % AHEAD][h] = g;
+          }
+        }
+      };
+      auto make = [&](int u, u32x4 (&w)[2]) {
+        union { float f[8]; u32x4 q[2]; } v;
+        const int r = u >> 1, j = u & 1;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v.f[c] = value(acc[r][2 * j + (c >> 2)][c & 3], sa[r], sw[j][c], bv[j][c]);
+        turn(v.q[0], v.q[1], 2 * kq, 2 * kq + 1, w);
+      };
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) load_x(u);
+      u32x4 w[2], nx[2];
+      make(0, w);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int n = nb + 32 * (u & 1);
+        if (u + 1 < U) make(u + 1, nx);
+        // (used here on every path: a load that some path leaves pending would be waited for in the next tile's loop)
+        if constexpr (RESID) asm volatile("" :: "v"(xr[u % AHEAD][0]), "v"(xr[u % AHEAD][1]), "v"(gr[u % AHEAD][0]), "v"(gr[u % AHEAD][1]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (row_in(u, h) && n < N) {
+            f32x4 x4;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              x4[c] = __uint_as_float(w[h][c]);
+              if constexpr (RESID) x4[c] = __builtin_fmaf(gr[u % AHEAD][h][c], x4[c], xr[u % AHEAD][h][c]);
+            }
+            float* xp = (float*)row_at(u, h);
+            if (n + 4 <= N) *(f32x4*)xp = x4;
+            else {
+#pragma unroll
+              for (int c = 0; c < 3; ++c)
+                if (n + c < N) xp[c] = x4[c];
+            }
+          }
+        }
+        if (u + AHEAD < U) load_x(u + AHEAD);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = nx[h];
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // Transposed columns: acc[2 i][c], acc[2 i + 1][c] hold rows 32 i + 8 kq + 0..7 of column 16 c + l16.  Units of 32 rows x 32
+    // columns; a lane writes 8 rows of a column as one 16-byte piece (at any 2-byte offset) when the 32 rows are neighbours
+    // in the transposed matrix, else in pairs and single elements.
+    auto transposed = [&]() {
+      typedef u32x4 u32x4_any __attribute__((aligned(2)));
+      const int nv0 = nw - P.vt_from, ldvt = P.ldvt;
+      const int* const map = P.vt_col;
+      bf16_t* const vt_out = P.vt;
+      float bv[CT], sw[CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const int n = nw + c * 16 + l16;
+        bv[c] = bias && n < N ? bias[n] : 0.f;
+        sw[c] = n < N ? P.sw[n] : 0.f;
+      }
+      const int fr = ln >> 2, fc = ln & 3;               // my column (and the one 16 on) and piece when a unit is read back
+      auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
+      const uint32_t voff = (uint32_t)(fr * ldvt + fc * 8) * 2u;
+#pragma unroll
+      for (int i = 0; i < RT / 2; ++i) {
+        const int mb = mw + i * 32;
+        float s8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s8[e] = row_scale(mb + kq * 8 + e);
+        bool consec = mb + 32 <= M;
+        int cb = 0;
+        if (consec) {
+          cb = map[mb];
+          consec = map[mb + 31] == cb + 31;
+        }
+        int col[8];
+        if (!consec) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) col[e] = mb + fc * 8 + e < M ? map[mb + fc * 8 + e] : -1;
+          asm volatile("" :: "v"(col[0]), "v"(col[1]), "v"(col[2]), "v"(col[3]), "v"(col[4]), "v"(col[5]), "v"(col[6]), "v"(col[7]));
+        }
+#pragma unroll
+        for (int cp = 0; cp < 2; ++cp) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int c = cp * 2 + q;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = value(acc[2 * i + (e >> 2)][c][e & 3], s8[e], sw[c], bv[c]);
+            const u32x4 w = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+            *(u32x4*)at(q * 16 + l16, kq) = w;
+          }
+          asm volatile("" ::: "memory");
+          u32x4 w[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) w[h] = *(const u32x4*)at(h * 16 + fr, fc);
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int f = cp * 32 + h * 16;
+            if (fr >= N - nw - f) continue;
+            if (consec) *(u32x4_any*)((char*)(vt_out + (size_t)(nv0 + f) * ldvt + cb) + voff) = w[h];
+            else {
+              bf16_t* dst = vt_out + (size_t)(nv0 + f + fr) * ldvt;
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                if (col[e + 1] == col[e] + 1 && (col[e] & 1) == 0) *(uint32_t*)(dst + col[e]) = w[h][e >> 1];
+                else {
+                  if (col[e] >= 0) dst[col[e]] = (bf16_t)w[h][e >> 1];
+                  if (col[e + 1] >= 0) dst[col[e + 1]] = (bf16_t)(w[h][e >> 1] >> 16);
+                }
+              }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    // gated pair: the wave's 64 columns are 32 of the gate (acc[.][0, 1]) and the same 32 of the values (acc[.][2, 3])
+    auto gated = [&]() {
+      const int nw2 = nw >> 1, ldc = P.ldc;
+      bf16_t* const out = (bf16_t*)P.out;
+      float sg[8], su[8];
+      load_cols(P.sw, nw2 + kq * 8, N, sg);
+      load_cols(P.sw2, nw2 + kq * 8, N, su);
+      load_sa();
+      const int fr = ln >> 2, fc = ln & 3;               // my row (and the one 16 on) and piece when 32 rows are read back
+      auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
+      const bool full = nw2 + fc * 8 + 8 <= N;
+      const uint32_t voff = (uint32_t)(fr * ldc + fc * 8) * 2u;
+#pragma unroll
+      for (int i = 0; i < RT / 2; ++i) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int r = 2 * i + q;
+          float v[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+            v[c] = gelu(value(acc[r][c >> 2][c & 3], sa[r], sg[c], 0.f)) * value(acc[r][2 + (c >> 2)][c & 3], sa[r], su[c], 0.f);
+          const u32x4 w = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+          *(u32x4*)at(q * 16 + l16, kq) = w;
+        }
+        asm volatile("" ::: "memory");
+        u32x4 w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = *(const u32x4*)at(h * 16 + fr, fc);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = i * 32 + h * 16;
+          char* const xp = (char*)(out + (size_t)(mw + k) * ldc + nw2) + voff;
+          if (fr < M - mw - k) {
+            if (full) *(u32x4*)xp = w[h];
+            else
+              for (int c = 0; c < N - nw2 - fc * 8; ++c) ((bf16_t*)xp)[c] = (bf16_t)(w[h][c >> 1] >> (16 * (c & 1)));
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (pair) { gated(); return; }
+    if (vt) { transposed(); return; }
+    if (P.kind == OUT_GELU_BF16) plain_bf16(std::true_type{});
+    else if (P.kind == OUT_BF16) plain_bf16(std::false_type{});
+    else if (P.kind == OUT_F32) plain_f32(std::false_type{});
+    else plain_f32(std::true_type{});
+  };
+
+  // ---- all my units ----------------------------------------------------------------------------------------------------
+  aim(ld_t);
+#pragma unroll
+  for (int st = 0; st < (NS == 2 ? 2 : NS - 1); ++st) {
+    if (st) advance();
+    issue_b(st); issue_a(st, A_FIRST, A_END);
   }
-  for (int i = 0; i < 2; ++i)
-    for (int j = 0; j < 2; ++j)
-      for (int e = 0; e < 4; ++e) {
-        const int m = m0 + i * 16 + kq * 4 + e, n = n0 + j * 16 + l16;
-        if (PAIR) put_pair(P, m, n, acc[i][j][e], acc2[i][j][e]);
-        else put(P, m, n, acc[i][j][e]);
-      }
+  wait_vm<(NS == 2 ? 1 : NS - 2) * LPS, false>();
+  wg_barrier();
+  for (int t = blockIdx.x >> 3; t < t_count; t += t_step) {
+    int tm, tn, k0, k1;
+    unit(t, tm, tn, k0, k1);
+    const bool vt = !pair && tn * BN >= P.vt_from;
+    if (vt) run(std::true_type{}, k1 - k0);
+    else run(std::false_type{}, k1 - k0);
+    if (splits > 1) {
+      // a share: the sums in register order, for the reduction
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      i32x4* const dst = (i32x4*)P.partial + ((size_t)(t_first + t) * 8 + wave) * (RT * CT * 64) + ln;
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) dst[(r * CT + c) * 64] = acc[r][c];
+    } else {
+      epilogue(tm, tn, vt);
+    }
+  }
+  wait_vm<0, true>();                        // drain the redundant tail loads before LDS is released
 }
 
-size_t gemm_i8_work_bytes(int, int, int, bool) { return 0; }
+// The shares of a split product added up, with the epilogue: a thread per four results.
+template <int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(256) void reduce_i8_kernel(const GemmI8 P) {
+  constexpr int RT = BM / WM / 16, CT = 4, CHUNK = 8 * RT * CT * 64;      // i32x4 of a share
+  const bool pair = P.W2 != nullptr;
+  const int per = pair ? CHUNK / 2 : CHUNK;
+  const int tile = blockIdx.x / (per / 256);
+  int q = (blockIdx.x % (per / 256)) * 256 + threadIdx.x;
+  const int lane = q & 63, l16 = lane & 15, kq = lane >> 4;
+  q >>= 6;
+  const int c = pair ? q % 2 : q % CT, r = (pair ? q / 2 : q / CT) % RT, wave = (pair ? q / 2 : q / CT) / RT;
+  const int wm = wave / WN, wn = wave % WN;
+  int tm, tn;
+  tile_coords(P, tile, tm, tn);
+  const bool vt = !pair && tn * BN >= P.vt_from;
+  const int mw = tm * BM + wm * (RT * 16), nw = tn * BN + wn * 64;
+  int m, n;
+  if (vt) { m = mw + (r >> 1) * 32 + kq * 8 + (r & 1) * 4; n = nw + c * 16 + l16; }
+  else { m = mw + r * 16 + l16; n = (pair ? nw >> 1 : nw) + (c >> 1) * 32 + kq * 8 + (c & 1) * 4; }
+  if (m >= P.M || n >= P.N) return;
+  auto sum = [&](int cc) {
+    const i32x4* p = (const i32x4*)P.partial + (size_t)tile * P.splits * CHUNK + ((wave * RT + r) * CT + cc) * 64 + lane;
+    i32x4 s = p[0];
+#pragma unroll 4
+    for (int k = 1; k < P.splits; ++k) s += p[(size_t)k * CHUNK];
+    return s;
+  };
+  const i32x4 s = sum(c);
+  if (pair) put_pair4(P, m, n, s, sum(c + 2));
+  else if (vt) put_col4(P, m, n, s);
+  else put_row4(P, m, n, s);
+}
+
+// ---- few rows: the weights as a stream ---------------------------------------------------------------------------------
+//
+// A workgroup owns 16 NT columns (of a pair: 8 NT of each product) and 16 MT rows.  Its waves take every WV-th slab of
+// 128 codes, so that together they read runs of WV * 128 bytes of every weight row, each exactly once.  Every wave has an LDS
+// ring of its own, D slabs deep, and waits for nobody: no barrier until the waves' sums meet in LDS.  One launch, no scratch.
+// Waves of a workgroup: as many slabs in flight as LDS holds (up to 8 for each wave); eight waves have 256 registers each, four have 512.
+constexpr int stream_waves(int mt, int nt) {
+  const int slab = (mt + nt) * 2048, regs = mt * nt * 4 + (mt + nt) * 10 + 24;
+  int best = 4, most = 0;
+  for (int w = regs <= 256 ? 8 : 4; w >= 4; --w) {
+    int d = 160 * 1024 / (w * slab);
+    if (d > 8) d = 8;
+    if (w * d > most) { most = w * d; best = w; }
+  }
+  return best;
+}
+template <int MT, int NT, bool PAIR>
+struct StreamShape {
+  static constexpr int L = (MT + NT) * 2, SLAB = L * 1024;     // loads of 1 KB and bytes of a slab
+  static constexpr int WV = stream_waves(MT, NT);
+  static constexpr int FIT = 160 * 1024 / (WV * SLAB), D = FIT > 8 ? 8 : FIT;
+  static constexpr int NC = PAIR ? NT / 2 : NT;                // 16-column tiles of one product
+  static constexpr int passes() { int p = 1; while (MT % p || WV * (MT / p) * NT > 160) ++p; return p; }
+  static constexpr int IP = MT / passes();                     // 16-row tiles whose sums meet in LDS at a time
+  static constexpr int RING = WV * D * SLAB, RED = WV * IP * NT * 1024, LDS = RING > RED ? RING : RED;
+  static_assert(D >= 1 && (D - 1) * L < 64 && (!PAIR || NT % 2 == 0), "ring");
+};
+template <int MT, int NT, bool PAIR>
+__global__ __launch_bounds__((StreamShape<MT, NT, PAIR>::WV * 64)) void stream_i8_kernel(const GemmI8 P) {
+  using S = StreamShape<MT, NT, PAIR>;
+  constexpr int L = S::L, D = S::D, WV = S::WV, NC = S::NC;
+  extern __shared__ __attribute__((aligned(128))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, kq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // XCD x (workgroup ids are dealt round-robin) takes a contiguous range of the tiles: the row tiles of one column tile
+  // together, or the other way round, whichever operand is larger is then read by one XCD alone
+  const int x = blockIdx.x & 7, T = gridDim.x;
+  const int tile = x * (T >> 3) + (x < (T & 7) ? x : (T & 7)) + (blockIdx.x >> 3);
+  const bool by_m = P.M > (PAIR ? 2 * P.N : P.N);
+  const int tm = by_m ? tile / P.tiles_n : tile % P.tiles_m, tn = by_m ? tile % P.tiles_n : tile / P.tiles_m;
+  const int m0 = tm * (MT * 16), n0 = tn * NC * 16;
+  unsigned char* const ring = smem + wave * (D * S::SLAB);
+  // byte offsets of my lane's 16 codes: load i fills slab rows 8 i .. 8 i + 7, rows of A first
+  uint32_t off[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const int r = i * 8 + (lane >> 3), c = ((lane & 7) ^ swz_key(r)) * 16;
+    if (i < 2 * MT) {
+      const int m = m0 + r < P.M ? r : P.M - 1 - m0;     // rows past the end repeat the last one and are not stored
+      off[i] = (uint32_t)m * (uint32_t)P.lda + c;
+    } else {
+      const int j = (r - 16 * MT) >> 4, n = n0 + (j % NC) * 16 + (r & 15);
+      off[i] = (uint32_t)((n < P.N ? n : P.N - 1) - n0) * (uint32_t)P.ldw + c;
+    }
+  }
+  const int8_t* const A = P.A + (size_t)m0 * P.lda;
+  const int8_t* const W = P.W + (size_t)n0 * P.ldw;
+  const int8_t* const W2 = PAIR ? P.W2 + (size_t)n0 * P.ldw : W;
+  const int nk = P.K / 128, mine = (nk - wave + WV - 1) / WV;            // slabs wave, wave + WV, ...
+  auto load = [&](int i, int s, int stage) {
+    buffer_load_lds16(i < 2 * MT ? A : (i - 2 * MT) / 2 < NC ? W : W2, (lptr_t)(ring + stage * S::SLAB + i * 1024), off[i], (wave + WV * s) * 128);
+  };
+  i32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  const int at = l16 * 128 + ((kq ^ swz_key(l16)) << 4);
+  // slab s, which has landed in `stage`; next: the stage is filled again with slab s + D, whose loads go out ahead of the products
+  auto multiply = [&](int s, int stage, auto next) {
+    const unsigned char* const p[2] = {ring + stage * S::SLAB + at, ring + stage * S::SLAB + (at ^ 64)};     // (odd tiles flip bit 2 of the key)
+    i32x4 fa[2][MT], fb[2][NT];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fb[h][j] = *(const i32x4*)(p[h ^ ((MT + j) & 1)] + (MT + j) * 2048);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[h][i] = *(const i32x4*)(p[h ^ (i & 1)] + i * 2048);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (in registers before the stage is loaded over)
+    __builtin_amdgcn_sched_barrier(0);
+    // the loads spread over the products: back to back a wave waits some 70 cycles for each to be taken
+    constexpr int NM = 2 * MT * NT, PER = NM / L > 1 ? NM / L / 2 : 1;
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      const int h = q / (MT * NT), i = q / NT % MT, j = q % NT;
+      if (decltype(next)::value && q % PER == 0 && q / PER < L) load(q / PER, s + D, stage);
+      acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0);
+    }
+    if constexpr (decltype(next)::value) {
+#pragma unroll
+      for (int i = (NM + PER - 1) / PER; i < L; ++i) load(i, s + D, stage);
+#pragma unroll
+      for (int i = 0; i < L && i * PER < NM; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int s = 0; s < D; ++s)
+    if (s < mine)
+#pragma unroll
+      for (int i = 0; i < L; ++i) load(i, s, s);
+  int s = 0, stage = 0;
+  for (; s + D < mine; ++s) {
+    wait_vm<(D - 1) * L, false>();                       // slab s
+    multiply(s, stage, std::true_type{});
+    stage = stage + 1 == D ? 0 : stage + 1;
+  }
+  for (; s < mine; ++s) {                                // the last D: fewer are in flight with every step
+    switch (mine - 1 - s) {
+      case 7: if constexpr (D > 7) wait_vm<(D > 7 ? 7 : 0) * L, false>(); break;
+      case 6: if constexpr (D > 6) wait_vm<(D > 6 ? 6 : 0) * L, false>(); break;
+      case 5: if constexpr (D > 5) wait_vm<(D > 5 ? 5 : 0) * L, false>(); break;
+      case 4: if constexpr (D > 4) wait_vm<(D > 4 ? 4 : 0) * L, false>(); break;
+      case 3: if constexpr (D > 3) wait_vm<(D > 3 ? 3 : 0) * L, false>(); break;
+      case 2: if constexpr (D > 2) wait_vm<(D > 2 ? 2 : 0) * L, false>(); break;
+      case 1: wait_vm<L, false>(); break;
+      default: wait_vm<0, false>(); break;
+    }
+    multiply(s, stage, std::false_type{});
+    stage = stage + 1 == D ? 0 : stage + 1;
+  }
+  // (16-byte place of a lane's sums inside their 16x16 tile: turned by the column group, so that reading along a row meets 16 banks of 16 bytes)
+  i32x4* const red = (i32x4*)smem;
+  auto place = [](int i, int j, int row, int q) { return (i * NT + j) * 64 + q * 16 + (row ^ ((j * 4 + q) & 15)); };
+  constexpr int IP = S::IP;
+  auto sum = [&](int q) {
+    i32x4 t = red[q];
+#pragma unroll
+    for (int w = 1; w < WV; ++w) t += red[q + w * IP * NT * 64];
+    return t;
+  };
+  const bool by_rows = n0 >= P.vt_from;                  // (transposed: neighbouring threads take neighbouring rows)
+#pragma unroll
+  for (int i0 = 0; i0 < MT; i0 += IP) {
+    __syncthreads();                                     // (the rings, or the sums before, are done with)
+#pragma unroll
+    for (int i = 0; i < IP; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) red[wave * (IP * NT * 64) + place(i, j, l16, kq)] = acc[i0 + i][j];
+    __syncthreads();
+    for (int q = tid; q < IP * NC * 64; q += WV * 64) {
+      const int row = by_rows ? q % (IP * 16) : q / (NC * 4), g = by_rows ? q / (IP * 16) : q % (NC * 4);
+      const int m = m0 + i0 * 16 + row, n = n0 + g * 4;
+      if (m >= P.M || n >= P.N) continue;
+      const int i = row >> 4, j = g >> 2;
+      if constexpr (PAIR) put_pair4(P, m, n, sum(place(i, j, row & 15, g & 3)), sum(place(i, j + NC, row & 15, g & 3)));
+      else put_row4(P, m, n, sum(place(i, j, row & 15, g & 3)));
+    }
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------
+namespace {
+
+template <int BM, int BN, int WM, int WN, int NS>
+void launch8(hipStream_t s, GemmI8& p) {
+  p.tiles_m = (p.M + BM - 1) / BM;
+  p.tiles_n = ((p.W2 ? 2 * p.N : p.N) + BN - 1) / BN;
+  constexpr int lds = NS * (BM + BN) * 128 + 8 * 2048;
+  static_assert(lds <= 160 * 1024, "LDS of a CU");
+  auto kern = gemm8_i8_kernel<BM, BN, WM, WN, NS>;
+  static std::atomic<unsigned> seen{0};
+  if (first_use_on_device(seen)) (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const int units = p.tiles_m * p.tiles_n * p.splits;
+  hipLaunchKernelGGL(kern, dim3(units < 256 ? units : 256), dim3(512), lds, s, p);
+  if (p.splits > 1) {
+    constexpr int per = 8 * (BM / WM / 16) * 4 * 64;
+    hipLaunchKernelGGL((reduce_i8_kernel<BM, BN, WM, WN>), dim3(p.tiles_m * p.tiles_n * ((p.W2 ? per / 2 : per) / 256)), dim3(256), 0, s, p);
+  }
+}
+
+template <int MT, int NT, bool PAIR>
+void launch_stream_t(hipStream_t s, GemmI8& p) {
+  using S = StreamShape<MT, NT, PAIR>;
+  auto kern = stream_i8_kernel<MT, NT, PAIR>;
+  static std::atomic<unsigned> seen{0};
+  if (first_use_on_device(seen)) (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+  p.tiles_m = (p.M + MT * 16 - 1) / (MT * 16);
+  p.tiles_n = (p.N + S::NC * 16 - 1) / (S::NC * 16);
+  hipLaunchKernelGGL(kern, dim3(p.tiles_m * p.tiles_n), dim3(S::WV * 64), S::LDS, s, p);
+}
+template <int MT>
+bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
+  if (p.W2) {
+    switch (nt) {
+      case 2: launch_stream_t<MT, 2, true>(s, p); return true;
+      case 4: launch_stream_t<MT, 4, true>(s, p); return true;
+      case 6: launch_stream_t<MT, 6, true>(s, p); return true;
+      case 8: if constexpr (MT >= 4 && MT <= 8) { launch_stream_t<MT, 8, true>(s, p); return true; }
+    }
+    return false;
+  }
+  switch (nt) {
+    case 1: launch_stream_t<MT, 1, false>(s, p); return true;
+    case 2: launch_stream_t<MT, 2, false>(s, p); return true;
+    case 3: launch_stream_t<MT, 3, false>(s, p); return true;
+    case 4: launch_stream_t<MT, 4, false>(s, p); return true;
+    case 6: if constexpr (MT >= 4) { launch_stream_t<MT, 6, false>(s, p); return true; }
+      return false;
+    case 8: if constexpr (MT >= 4 && MT <= 8) { launch_stream_t<MT, 8, false>(s, p); return true; }
+  }
+  return false;
+}
+bool launch_stream(hipStream_t s, GemmI8& p, int mt, int nt) {
+  p.splits = 1;
+  switch (mt) {
+    case 1: return launch_stream_m<1>(s, p, nt);
+    case 2: return launch_stream_m<2>(s, p, nt);
+    case 3: return launch_stream_m<3>(s, p, nt);
+    case 4: return launch_stream_m<4>(s, p, nt);
+    case 5: return launch_stream_m<5>(s, p, nt);
+    case 6: return launch_stream_m<6>(s, p, nt);
+    case 8: return launch_stream_m<8>(s, p, nt);
+  }
+  return false;
+}
+
+// ---- the choice of tile ----
+// Estimated time of a product in microseconds: the rounds of 256 workgroups, in each the slabs of one tile at a measured rate, and a fixed
+// part.  A slab of a stream tile takes what a CU pulls (85 GB/s) and a share of its products; of an 8-wave tile 0.5, 0.8 and 1.3 us
+// (1.42 where every CU has one and the clock falls).  Nothing is faster than its bytes at 4.8 TB/s.
+// Over 96 products of 1 to 4096 rows, 64 to 12288 columns and K from 256 to 10240, every candidate timed, the one chosen took 1.015 times the
+// best one's time in the mean and never more than 1.4 times.  What both sides take near the borders: 200 rows, N = 12288, K = 4096 stream
+// 23.8, 128x128 24.6; 333 rows 35.7 and 128x256 34.1; 1000 rows, N = 4096, K = 10240 stream 45.1, 128x128 54; 500 rows 31.8, 256x128 in four
+// shares 36; 128 rows, N = 4096, K = 4096 stream 7.6, 128x128 in four shares 16.9.
+struct Choice { int variant, splits; float us; };
+
+Choice choose(int M, int N, int K, bool pair, size_t scratch) {
+  const int nk = K / 128;
+  const long long cols = pair ? 2LL * N : N;
+  const float least = 3.5f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
+  Choice best = {0, 1, 1e30f};
+  auto offer = [&](int variant, int splits, float us) {
+    if (us < least) us = least + us * 1e-3f;
+    if (us < best.us) best = Choice{variant, splits, us};
+  };
+  for (int mt : {1, 2, 3, 4, 5, 6, 8})
+    for (int nt : {1, 2, 3, 4, 6, 8}) {
+      if ((pair && nt % 2) || (nt > 4 && mt < 4 && !(pair && nt == 6))) continue;
+      const long long wgs = (long long)((M + 16 * mt - 1) / (16 * mt)) * ((cols + 16 * nt - 1) / (16 * nt));
+      const long long rounds = (wgs + 255) / 256;
+      offer(100 * mt + nt, 1, 2.5f + (float)rounds * (nk * (0.0241f * (mt + nt) + 0.0022f * mt * nt) + (rounds > 1 ? 4.f : 2.f) + 0.03f * mt * nt));
+    }
+  const struct { int bm, bn; float slab, full, fixed; } tiles[] = {{128, 128, 0.5f, 0.5f, 6.5f}, {128, 256, 0.8f, 0.86f, 7.f},
+                                                                  {256, 128, 0.8f, 0.86f, 7.f}, {256, 256, 1.28f, 1.42f, 8.f}};
+  for (const auto& t : tiles) {
+    const long long n = (long long)((M + t.bm - 1) / t.bm) * ((cols + t.bn - 1) / t.bn);
+    offer(t.bm * 1000 + t.bn, 1, 3.f + (float)((n + 255) / 256) * (nk * (n >= 256 ? t.full : t.slab) + t.fixed));
+    // shares of K: one round of them, their sums through memory and a second launch
+    for (int s = 2; s <= 8 && n * s <= 256 && nk / s >= 8; ++s)
+      if ((size_t)n * s * t.bm * t.bn * 4 <= scratch)
+        offer(t.bm * 1000 + t.bn, s, 12.f + (nk + s - 1) / s * t.slab + t.fixed * 0.7f + (float)n * s * t.bm * t.bn / 1e6f);
+  }
+  return best;
+}
+
+}  // namespace
+
+size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {
+  const Choice c = choose(M, N, K, pair, ~(size_t)0);
+  if (c.splits == 1) return 0;
+  const int bm = c.variant / 1000, bn = c.variant % 1000;
+  return (size_t)((M + bm - 1) / bm) * (((pair ? 2LL * N : N) + bn - 1) / bn) * c.splits * bm * bn * 4;
+}
+
+// variant 100 MT + NT: a stream tile; BM*1000 + BN: an 8-wave tile with p.splits shares
+int launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant) {
+  if (variant < 1000) return launch_stream(s, p, variant / 100, variant % 100) ? variant : -1;
+  if (variant == 256256) launch8<256, 256, 2, 4, 2>(s, p);
+  else if (variant == 256128) launch8<256, 128, 4, 2, 3>(s, p);
+  else if (variant == 128256) launch8<128, 256, 2, 4, 3>(s, p);
+  else if (variant == 128128) launch8<128, 128, 4, 2, 4>(s, p);
+  else return -1;
+  return variant;
+}
 
 void launch_gemm_i8(hipStream_t s, GemmI8& p) {
-  const dim3 grid((p.N + 63) / 64, (p.M + 63) / 64);
-  if (p.W2) hipLaunchKernelGGL(gemm_i8_simple_kernel<true>, grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(gemm_i8_simple_kernel<false>, grid, dim3(256), 0, s, p);
+  const Choice c = choose(p.M, p.N, p.K, p.W2 != nullptr, p.partial ? p.partial_bytes : 0);
+  p.splits = c.splits;
+  launch_gemm_i8_variant(s, p, c.variant);
+}
+
+int gemm_i8_choice(int M, int N, int K, bool pair, size_t scratch, int* splits) {
+  const Choice c = choose(M, N, K, pair, scratch);
+  *splits = c.splits;
+  return c.variant;
 }
 
 }  // namespace dit

@@ -9,12 +9,16 @@ inline bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 inline int rup128(int n) { return (n + 127) / 128 * 128; }
 inline dit_status launched() { return hipGetLastError() == hipSuccess ? DIT_OK : DIT_EDEVICE; }
 
+// (tiles and shares are counted in 32 bits)
+inline bool countable(int M, int N) { return (M + 127LL) / 128 * ((N + 15LL) / 16) < (1LL << 26); }
+
 // what the three forms of the product have in common
 dit_status check_product(const void* A, int lda, const float* a_scale, const void* W, int ldw, const float* w_scale, int M, int N, int K,
                          const void* out, const void* work) {
   if (!A || !a_scale || !W || !w_scale || !out) return DIT_EINVAL;
   if (M < 0 || N < 0 || K <= 0 || K % 128 || K > DIT_I8_MAX_K || lda < K || ldw < K || lda % 16 || ldw % 16) return DIT_ESHAPE;
-  if (lda >= (1 << 22) || ldw >= (1 << 22) || M > (1 << 24) || N > (1 << 24)) return DIT_ESHAPE;   // 32-bit offsets inside a tile; tile counts
+  if (lda >= (1 << 22) || ldw >= (1 << 22)) return DIT_ESHAPE;                       // 32-bit offsets inside a tile
+  if (!countable(M, N)) return DIT_ESHAPE;
   if (off16(A) || off16(W) || off16(out) || off16(work)) return DIT_ESHAPE;
   return DIT_OK;
 }
@@ -98,7 +102,7 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
 }
 
 size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair) {
-  if (M <= 0 || N <= 0 || K <= 0 || K % 128 || K > DIT_I8_MAX_K || M > (1 << 24) || N > (1 << 24)) return 0;
+  if (M <= 0 || N <= 0 || K <= 0 || K % 128 || K > DIT_I8_MAX_K || !countable(M, N)) return 0;
   return gemm_i8_work_bytes(M, N, K, pair != 0);
 }
 

@@ -26,6 +26,7 @@ struct GemmI8 {
   size_t partial_bytes;
 };
 void launch_gemm_i8(hipStream_t s, GemmI8& p);
+int launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant);
 size_t gemm_i8_work_bytes(int M, int N, int K, bool pair);
 
 }  // namespace dit
