@@ -65,6 +65,25 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
 /* Scratch of one such call (pair != 0: dit_op_gemm_i8_geglu); 0 where nothing is split or the arguments are refused. */
 size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair);
 
+/* ---- the Encode stage in 8 bits ------------------------------------------------------- */
+
+/* enc_forward (encoder.h) with its matrix products on codes: weights with a scale per output channel, their inputs with one per token.
+ * The residual stream and the norms' statistics are as there (float32, 64 bits), attention runs on bf16, a branch is rounded to bf16 before
+ * the next norm adds it (the last one is added in float32).
+ *
+ * enc_i8_quantize writes the codes of every matrix of the bound weight arena to dev_codes (256-byte aligned, enc_i8_weight_bytes), which the
+ * context refers to from then on; the arena stays in use (embedding, bias table, gains).  It has to be called again after
+ * enc_init_weights, enc_set_tensor of a matrix and a bind of another arena, after which enc_i8_forward refuses with DIT_EINVAL, and after the
+ * arena has been written by other means.
+ * DIT_EUNSUPPORTED for matrices with more than DIT_I8_MAX_ROW inputs.
+ * enc_i8_forward: arguments, results and streams of enc_forward; the workspace bound with enc_bind must have
+ * enc_i8_workspace_bytes.  Capture points: those of enc_set_tap but "l<i>.ln1", which is never reached.
+ * A sequence's result is the same, bit for bit, whatever it is packed with. */
+size_t enc_i8_weight_bytes(const enc_ctx* ctx);
+size_t enc_i8_workspace_bytes(const enc_ctx* ctx, int n_seq, const int* lens);
+dit_status enc_i8_quantize(enc_ctx* ctx, void* dev_codes, size_t bytes);
+dit_status enc_i8_forward(enc_ctx* ctx, int n_seq, const int* lens, const int* dev_tokens, void* dev_out_bf16, float* dev_out_f32);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,8 +1,8 @@
 // Host runtime of the Encode stage (T5-v1.1-style text encoder): tensor table, workspace
 // layout and the launch sequence of one forward pass.  Every arithmetic step runs in the
 // kernels of gemm.hip, attention.hip, elementwise.hip and encoder.hip.
-#include "../../include/encoder.h"
-#include "dit_internal.h"
+#include "../../include/int8.h"
+#include "int8_internal.h"
 
 #include <algorithm>
 #include <cmath>
@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <cstring>
 #include <map>
+#include <new>
 #include <string>
 #include <unordered_map>
 #include <vector>
@@ -41,6 +42,8 @@ struct enc_ctx {
   std::map<std::string, ETap> taps;
   std::vector<unsigned char> host_meta;        // kept alive until the upload has been consumed
   hipEvent_t meta_done = nullptr;
+  unsigned char* codes = nullptr;  // the matrices in 8 bits (enc_i8_quantize)
+  bool codes_valid = false;        // ... and they are those of the bound weights
   bool launch_refused = false;     // a product of the running call was outside the GEMM's limits
 };
 
@@ -189,6 +192,47 @@ dit_status tap(enc_ctx* c, const std::string& name, const void* src, size_t byte
     }                                                                     \
   } while (0)
 
+
+// ---- in 8 bits ----
+// Codes of one layer, one behind the other: query, key and value rows as one matrix, output, gate, up and output of the MLP; then
+// the scales of all of these rows.  (Widths are multiples of 256: no padding, every part 256-byte aligned.)
+struct Codes { size_t qkv, o, wi0, wi1, wo, s_qkv, s_o, s_wi0, s_wi1, s_wo, bytes; };
+Codes codes_of_layer(const enc_config& g) {
+  const size_t d = g.d_model, inner = (size_t)g.n_heads * g.head_dim, ff = g.d_ff;
+  size_t o = 0;
+  auto take = [&](size_t n) { const size_t at = o; o += rup(n, 256); return at; };
+  Codes c;
+  c.qkv = take(3 * inner * d); c.o = take(d * inner); c.wi0 = take(ff * d); c.wi1 = take(ff * d); c.wo = take(d * ff);
+  c.s_qkv = take(3 * inner * 4); c.s_o = take(d * 4); c.s_wi0 = take(ff * 4); c.s_wi1 = take(ff * 4); c.s_wo = take(d * 4);
+  c.bytes = o;
+  return c;
+}
+
+// bias_L: rounded up to whole tiles of 64 keys, so that the pad keys of a sequence's last tile have a place of their own in the bias
+// table too and what they round away does not depend on the longest sequence of the call.
+struct Layout8 { Layout base; int bias_L; size_t x, h, hs, qk, vt, o, q, qs, delta, act, bias, partial, partial_bytes, total; };
+void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector<unsigned char>* meta) {
+  const enc_config& g = c->cfg;
+  plan(c, n_seq, lens, L.base, meta);
+  const size_t M = L.base.M, d = g.d_model, inner = (size_t)g.n_heads * g.head_dim, ff = g.d_ff;
+  size_t o = L.base.x;                            // (behind the index data)
+  auto take = [&](size_t bytes) { const size_t at = o; o += rup(bytes, 256); return at; };
+  L.x = take(M * d * 4);
+  L.h = take(M * d); L.hs = take(M * 4);
+  L.qk = take(M * 2 * inner * 2);
+  L.vt = take(inner * (size_t)L.base.cols_pad * 2);
+  L.o = take(M * inner * 2);
+  L.q = take(M * std::max(inner, ff)); L.qs = take(M * 4);        // codes of the attention's output, then of the gated activation
+  L.delta = take(M * d * 2);
+  L.act = take(M * ff * 2);
+  L.bias_L = (int)rup(L.base.L, 64);
+  L.bias = take((size_t)g.n_heads * (2 * (size_t)L.bias_L - 1) * 4);
+  L.partial_bytes = std::max(std::max(gemm_i8_work_bytes((int)M, (int)(3 * inner), (int)d, false), gemm_i8_work_bytes((int)M, (int)d, (int)inner, false)),
+                             std::max(gemm_i8_work_bytes((int)M, (int)ff, (int)d, true), gemm_i8_work_bytes((int)M, (int)d, (int)ff, false)));
+  L.partial = take(L.partial_bytes);
+  L.total = o;
+}
+
 }  // namespace
 
 extern "C" {
@@ -244,6 +288,7 @@ dit_status enc_bind(enc_ctx* c, void* w, size_t wb, void* ws, size_t wsb) {
   if (!w || !ws) return efail(c, DIT_EINVAL, "null buffer");
   if (((uintptr_t)w & 255) || ((uintptr_t)ws & 255)) return efail(c, DIT_EINVAL, "buffers must be 256-byte aligned");
   if (wb < c->weight_bytes) return efail(c, DIT_ENOMEM, "weight arena has %zu bytes, needs %zu", wb, c->weight_bytes);
+  if (c->weights != w) c->codes_valid = false;
   c->weights = (unsigned char*)w; c->ws = (unsigned char*)ws; c->ws_bytes = wsb;
   return DIT_OK;
 }
@@ -253,6 +298,7 @@ dit_status enc_init_weights(enc_ctx* c, uint64_t seed, float std) {
   if (!c->weights) return efail(c, DIT_EINVAL, "enc_bind has not been called");
   if (!(std >= 0.f) || !std::isfinite(std)) return efail(c, DIT_EINVAL, "std must be finite and non-negative");
   EHIP(c, hipSetDevice(c->device));
+  c->codes_valid = false;
   EHIP(c, hipMemsetAsync(c->weights, 0, c->weight_bytes, c->stream));
   for (const ETensor& t : c->tensors) {
     const uint64_t key = mix(seed ^ (fnv(t.name) * 0x9E3779B97F4A7C15ull));
@@ -285,6 +331,7 @@ dit_status enc_set_tensor(enc_ctx* c, const char* name, const float* src, size_t
   EHIP(c, hipSetDevice(c->device));
   EHIP(c, hipStreamSynchronize(c->stream));
   if (t->kind == 0) {
+    c->codes_valid = false;
     std::vector<uint16_t> buf((size_t)t->rows_pad * t->ld, 0);
     for (int i = 0; i < t->rows_in; ++i)
       for (int o = 0; o < t->cols_out; ++o) buf[(size_t)o * t->ld + i] = h_f2bf(src[(size_t)i * t->cols_out + o]);
@@ -391,6 +438,132 @@ dit_status enc_forward(enc_ctx* c, int n_seq, const int* lens, const int* tokens
   if (c->launch_refused) return efail(c, DIT_ESHAPE, "a matrix product of this call is outside the GEMM kernels' limits");
   EHIP(c, hipGetLastError());
   return DIT_OK;
+}
+
+size_t enc_i8_weight_bytes(const enc_ctx* c) { return c ? codes_of_layer(c->cfg).bytes * c->cfg.n_layers : 0; }
+
+size_t enc_i8_workspace_bytes(const enc_ctx* c, int n_seq, const int* lens) {
+  if (!c || !lens_ok(n_seq, lens)) return 0;
+  try {
+    Layout8 L;
+    plan8(c, n_seq, lens, L, nullptr);
+    return L.total;
+  } catch (const std::bad_alloc&) { return 0; }
+}
+
+dit_status enc_i8_quantize(enc_ctx* c, void* dev_codes, size_t bytes) {
+  if (!c) return DIT_EINVAL;
+  if (!c->weights) return efail(c, DIT_EINVAL, "enc_bind has not been called");
+  if (!dev_codes || ((uintptr_t)dev_codes & 255)) return efail(c, DIT_EINVAL, "the codes' buffer is null or not 256-byte aligned");
+  if (bytes < enc_i8_weight_bytes(c)) return efail(c, DIT_ENOMEM, "the codes' buffer has %zu bytes, needs %zu", bytes, enc_i8_weight_bytes(c));
+  const enc_config& g = c->cfg;
+  const int d = g.d_model, inner = g.n_heads * g.head_dim, ff = g.d_ff;
+  if (std::max(std::max(d, inner), ff) > DIT_I8_MAX_ROW) return efail(c, DIT_EUNSUPPORTED, "rows of more than %d columns have no codes", (int)DIT_I8_MAX_ROW);
+  EHIP(c, hipSetDevice(c->device));
+  c->codes_valid = false;
+  const Codes k = codes_of_layer(g);
+  try {
+    for (int l = 0; l < g.n_layers; ++l) {
+      const std::string p = "l" + std::to_string(l);
+      unsigned char* at = (unsigned char*)dev_codes + k.bytes * l;
+      auto code = [&](const char* name, size_t codes, size_t scales, int row0, int rows, int cols) {
+        launch_quantize_i8(c->stream, Wm(c, p + name), false, Wld(c, p + name), rows, cols, (int8_t*)at + codes + (size_t)row0 * cols, cols,
+                           (float*)(at + scales) + row0);
+      };
+      code(".q.w", k.qkv, k.s_qkv, 0, inner, d); code(".k.w", k.qkv, k.s_qkv, inner, inner, d); code(".v.w", k.qkv, k.s_qkv, 2 * inner, inner, d);
+      code(".o.w", k.o, k.s_o, 0, d, inner);
+      code(".wi0.w", k.wi0, k.s_wi0, 0, ff, d); code(".wi1.w", k.wi1, k.s_wi1, 0, ff, d);
+      code(".wo.w", k.wo, k.s_wo, 0, d, ff);
+    }
+  } catch (const std::bad_alloc&) { return efail(c, DIT_ENOMEM, "out of host memory"); }
+  EHIP(c, hipGetLastError());
+  c->codes = (unsigned char*)dev_codes;
+  c->codes_valid = true;
+  return DIT_OK;
+}
+
+static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* tokens, void* out_bf16, float* out_f32) {
+  const enc_config& g = c->cfg;
+  EHIP(c, hipSetDevice(c->device));
+  // the previous call's host image must have been consumed before it is rebuilt
+  if (c->meta_done) EHIP(c, hipEventSynchronize(c->meta_done));
+  else EHIP(c, hipEventCreateWithFlags(&c->meta_done, hipEventDisableTiming));
+  Layout8 L;
+  plan8(c, n_seq, lens, L, &c->host_meta);
+  if (L.total > c->ws_bytes) return efail(c, DIT_ENOMEM, "workspace has %zu bytes, this call needs %zu", c->ws_bytes, L.total);
+  hipStream_t s = c->stream;
+  unsigned char* ws = c->ws;
+  EHIP(c, hipMemcpyAsync(ws + L.base.meta, c->host_meta.data(), c->host_meta.size(), hipMemcpyHostToDevice, s));
+  EHIP(c, hipEventRecord(c->meta_done, s));
+
+  const int M = L.base.M, d = g.d_model, H = g.n_heads, dh = g.head_dim, inner = H * dh, ff = g.d_ff;
+  float* x = (float*)(ws + L.x);
+  int8_t* h = (int8_t*)(ws + L.h); float* hs = (float*)(ws + L.hs);
+  bf16_t* qk = (bf16_t*)(ws + L.qk);
+  bf16_t* vt = (bf16_t*)(ws + L.vt); bf16_t* o = (bf16_t*)(ws + L.o);
+  int8_t* q8 = (int8_t*)(ws + L.q); float* qs = (float*)(ws + L.qs);
+  bf16_t* delta = (bf16_t*)(ws + L.delta); bf16_t* act = (bf16_t*)(ws + L.act);
+  float* bias = (float*)(ws + L.bias);
+  const unsigned char* meta = ws + L.base.meta;
+  const Codes k = codes_of_layer(g);
+  auto product = [&](const int8_t* A, int K, const float* sa, const unsigned char* at, size_t codes, size_t scales, int N, int kind, void* out, int ldc) {
+    GemmI8 p = {};
+    p.A = A; p.lda = K; p.sa = sa; p.W = (const int8_t*)at + codes; p.ldw = K; p.sw = (const float*)(at + scales);
+    p.M = M; p.N = N; p.K = K; p.kind = kind; p.out = out; p.ldc = ldc; p.vt_from = N;
+    p.partial = (int*)(ws + L.partial); p.partial_bytes = L.partial_bytes;
+    return p;
+  };
+
+  launch_embed_gather(s, tokens, Wv(c, "embed"), x, M, d, g.vocab);
+  launch_rel_bias_table(s, Wv(c, "rel_bias"), bias, H, L.bias_L);
+  // (pad columns of the transposed values: no product writes them)
+  launch_fill_u16(s, vt, (long long)inner * L.base.cols_pad, 0);
+  for (int l = 0; l < g.n_layers; ++l) {
+    const std::string p = "l" + std::to_string(l);
+    const unsigned char* at = c->codes + k.bytes * l;
+    launch_rmsnorm_i8(s, x, d, l ? delta : nullptr, false, d, Wv(c, p + ".ln1.g"), 1e-6f, M, d, l ? x : nullptr, d, h, d, hs);
+    if (l) ETAP("l" + std::to_string(l - 1) + ".x_out", x, (size_t)M * d * 4);
+    GemmI8 qkv = product(h, d, hs, at, k.qkv, k.s_qkv, 3 * inner, OUT_BF16, qk, 2 * inner);
+    qkv.vt_from = 2 * inner; qkv.vt = vt; qkv.ldvt = L.base.cols_pad; qkv.vt_col = (const int*)(meta + L.base.o_vt_col);
+    launch_gemm_i8(s, qkv);
+    AttnArgs a;
+    a.q = qk; a.ldq = 2 * inner; a.k = qk + inner; a.ldk = 2 * inner; a.vt = vt; a.ldvt = L.base.cols_pad; a.o = o; a.ldo = inner;
+    a.n_heads = H; a.head_dim = dh; a.cu_q = a.cu_k = (const int*)(meta + L.base.o_cu); a.vt_off = (const int*)(meta + L.base.o_vt_off);
+    a.tiles = (const AttnTile*)(meta + L.base.o_tiles); a.n_tiles = L.base.n_tiles; a.q_per_tile = 128; a.o_row_map = nullptr;
+    a.scale_log2 = 1.4426950408889634f;      // scores are not divided by sqrt(head_dim) in this encoder
+    a.mode = 3; a.bias = bias; a.bias_L = L.bias_L;
+    launch_attention(s, a);
+    ETAP(p + ".attn", o, (size_t)M * inner * 2);
+    launch_quantize_i8(s, o, false, inner, M, inner, q8, inner, qs);
+    GemmI8 po = product(q8, inner, qs, at, k.o, k.s_o, d, OUT_BF16, delta, d);
+    launch_gemm_i8(s, po);
+    launch_rmsnorm_i8(s, x, d, delta, false, d, Wv(c, p + ".ln2.g"), 1e-6f, M, d, x, d, h, d, hs);
+    ETAP(p + ".x_attn", x, (size_t)M * d * 4);
+    GemmI8 in = product(h, d, hs, at, k.wi0, k.s_wi0, ff, OUT_BF16, act, ff);
+    in.W2 = (const int8_t*)at + k.wi1; in.sw2 = (const float*)(at + k.s_wi1);
+    launch_gemm_i8(s, in);
+    ETAP(p + ".act", act, (size_t)M * ff * 2);
+    launch_quantize_i8(s, act, false, ff, M, ff, q8, ff, qs);
+    // the next layer's norm adds the branch; the last one goes straight into the residual
+    const bool last = l + 1 == g.n_layers;
+    GemmI8 out = product(q8, ff, qs, at, k.wo, k.s_wo, d, last ? OUT_RESID_F32 : OUT_BF16, last ? (void*)x : (void*)delta, d);
+    launch_gemm_i8(s, out);
+    if (last) ETAP(p + ".x_out", x, (size_t)M * d * 4);
+  }
+  launch_rmsnorm(s, x, Wv(c, "final.g"), (bf16_t*)out_bf16, out_f32, M, d);
+  EHIP(c, hipGetLastError());
+  return DIT_OK;
+}
+
+dit_status enc_i8_forward(enc_ctx* c, int n_seq, const int* lens, const int* tokens, void* out_bf16, float* out_f32) {
+  if (!c) return DIT_EINVAL;
+  if (!c->weights || !c->ws) return efail(c, DIT_EINVAL, "enc_bind has not been called");
+  if (!c->codes_valid) return efail(c, DIT_EINVAL, "the weights have no codes: enc_i8_quantize has not been called since they changed");
+  if (!tokens || (!out_bf16 && !out_f32)) return efail(c, DIT_EINVAL, "null tokens or no output buffer");
+  if (!lens_ok(n_seq, lens)) return efail(c, DIT_ESHAPE, "1..4096 sequences of 1..%d tokens, at most 2^20 tokens", (int)ENC_MAX_LEN);
+  try {
+    return forward_i8(c, n_seq, lens, tokens, out_bf16, out_f32);
+  } catch (const std::bad_alloc&) { return efail(c, DIT_ENOMEM, "out of host memory"); }
 }
 
 }  // extern "C"

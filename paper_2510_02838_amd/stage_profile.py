@@ -24,7 +24,7 @@ each for the stages before and after it:
           the bytes held (the paper: Encode and Decode are memory-bound and can reach a higher
           peak memory than Diffuse).
 
-    python -m paper_2510_02838_amd.stage_profile encode [--encoder t5_xxl] [--lens 32,128,500] [--max-batch 64]
+    python -m paper_2510_02838_amd.stage_profile encode [--encoder t5_xxl] [--lens 32,128,500] [--max-batch 64] [--int8]
     python -m paper_2510_02838_amd.stage_profile decode [--decoder ae_kl] [--res 128,256,512,1024] [--max-batch 8]
     python -m paper_2510_02838_amd.stage_profile decode --decoder vae3d [--res 256x384,512x768] [--frames 1,5,13]
           (the causal video decoder, one video per call: latency against the number of latent frames)
@@ -180,10 +180,16 @@ def run_encode(args):
     arch = synth.ENCODERS[args.encoder]
     lens_list = [int(v) for v in args.lens.split(",")]
     batches = [b for b in (1, 2, 4, 8, 16, 32, 64, 128) if b <= args.max_batch]
-    m = X.Encoder(arch)
+    if args.int8:
+        from . import int8
+        m = int8.EncoderI8(arch)
+    else:
+        m = X.Encoder(arch)
     m.ensure_workspace([max(lens_list)] * max(batches))
     m.init_weights(1, 0.02)
-    wbytes = m.weight_bytes()
+    if args.int8:
+        m.quantize()
+    wbytes = m.code_bytes() if args.int8 else m.weight_bytes()
     floor_ms = wbytes / 8e12 * 1e3
     rows = []
     for n in lens_list:
@@ -204,7 +210,7 @@ def run_encode(args):
             if not bool(torch.isfinite(out.float()).all().item()):
                 raise RuntimeError("non-finite encoder output")
             lat[b] = best
-            row = {"table": "encode", "encoder": args.encoder, "prompt_tokens": n, "batch": b, "ms": best * 1e3,
+            row = {"table": "encode", "encoder": args.encoder, "products": "int8" if args.int8 else "bf16", "prompt_tokens": n, "batch": b, "ms": best * 1e3,
                    "latency_vs_b1": best / lat[1], "prompts_per_s": b / best, "tokens_per_s": b * n / best,
                    "weight_read_floor_ms": floor_ms}
             rows.append(row)
@@ -522,6 +528,7 @@ def main():
     ap.add_argument("--frames", default="1,5,13", help="decode with a video decoder: latent frames per video")
     ap.add_argument("--encoder", default="t5_xxl", choices=["t5_xxl", "t5_tiny"])
     ap.add_argument("--lens", default="32,128,500")
+    ap.add_argument("--int8", action="store_true", help="encode: the products on 8-bit integers")
     ap.add_argument("--workload", default="sd3", choices=["sd3", "flux", "wan", "tiny"])
     ap.add_argument("--res", default=None)
     ap.add_argument("--steps", type=int, default=None, help="denoising steps per timed sample")
