@@ -32,37 +32,61 @@ __device__ __forceinline__ float gelu(float x) {
 }
 __device__ __forceinline__ float value(int acc, float sa, float sw, float bias) { return __builtin_fmaf((float)acc, sa * sw, bias); }
 
-// Four neighbouring columns of a row to their places (n + 3 may be past the end); up: the same columns of a pair's second product.
+// four neighbouring values of a vector at any place, those past the end are 0
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+__device__ __forceinline__ f32x4 load4(const float* p, int left) {
+  if (left >= 4) return *(const f32x4_any*)p;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < 3; ++c)
+    if (c < left) v[c] = p[c];
+  return v;
+}
+
+// What the epilogue needs for four neighbouring columns of a row (n + 3 may be past the end), fetched ahead of the sums: scales,
+// second scales or bias, the row's request or column of the transposed matrix, and for a residual what is there and the gate.
+struct Ahead { float sa; f32x4 sw, more, x, g; int map; };
+template <bool PAIR, class P>
+__device__ __forceinline__ Ahead fetch4(const P& p, int m, int n) {
+  const int left = p.N - n;
+  Ahead a;
+  a.sa = p.sa[m];
+  a.sw = load4(p.sw + n, left);
+  a.more = f32x4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (PAIR) a.more = load4(p.sw2 + n, left);
+  else {
+    if (p.bias) a.more = load4(p.bias + n, left);
+    const int* const map = n >= p.vt_from ? p.vt_col : p.row_req;
+    a.map = map ? map[m] : 0;
+    if (p.kind == OUT_RESID_F32) {
+      a.x = load4((const float*)p.out + (size_t)m * p.ldc + n, left);
+      a.g = f32x4{1.f, 1.f, 1.f, 1.f};
+      if (p.gate) a.g = load4(p.gate + (size_t)a.map * p.gate_stride + n, left);
+    }
+  }
+  return a;
+}
+// the four results to their places; up: the same columns of a pair's second product
 template <class P>
-__device__ __forceinline__ void put_row4(const P& p, int m, int n, const i32x4& acc) {
-  const float sa = p.sa[m];
-  const int left = p.N - n < 4 ? p.N - n : 4;
+__device__ __forceinline__ void put_row4(const P& p, int m, int n, const i32x4& acc, const Ahead& a) {
+  const int left = p.N - n;
   float v[4];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int k = c < left ? n + c : n;
-    v[c] = value(acc[c], sa, p.sw[k], p.bias ? p.bias[k] : 0.f);
-  }
+  for (int c = 0; c < 4; ++c) v[c] = value(acc[c], a.sa, a.sw[c], a.more[c]);
   if (n >= p.vt_from) {
-    const int col = p.vt_col[m];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      if (c < left) p.vt[(size_t)(n + c - p.vt_from) * p.ldvt + col] = bf(v[c]);
+      if (c < left) p.vt[(size_t)(n + c - p.vt_from) * p.ldvt + a.map] = bf(v[c]);
     return;
   }
   const size_t o = (size_t)m * p.ldc + n;
   if (p.kind == OUT_F32 || p.kind == OUT_RESID_F32) {
     float* out = (float*)p.out + o;
     if (p.kind == OUT_RESID_F32) {
-      const float* g = p.gate ? p.gate + (size_t)(p.row_req ? p.row_req[m] : 0) * p.gate_stride + n : nullptr;
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      if (left == 4) x = *(const f32x4*)out;
-      else
-        for (int c = 0; c < left; ++c) x[c] = out[c];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(g ? g[c < left ? c : 0] : 1.f, v[c], x[c]);
+      for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(a.g[c], v[c], a.x[c]);
     }
-    if (left == 4) *(f32x4*)out = f32x4{v[0], v[1], v[2], v[3]};
+    if (left >= 4) *(f32x4*)out = f32x4{v[0], v[1], v[2], v[3]};
     else
       for (int c = 0; c < left; ++c) out[c] = v[c];
   } else {
@@ -71,23 +95,19 @@ __device__ __forceinline__ void put_row4(const P& p, int m, int n, const i32x4& 
 #pragma unroll
       for (int c = 0; c < 4; ++c) v[c] = gelu(v[c]);
     }
-    if (left == 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    if (left >= 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
     else
       for (int c = 0; c < left; ++c) out[c] = bf(v[c]);
   }
 }
 template <class P>
-__device__ __forceinline__ void put_pair4(const P& p, int m, int n, const i32x4& gate, const i32x4& up) {
-  const float sa = p.sa[m];
-  const int left = p.N - n < 4 ? p.N - n : 4;
+__device__ __forceinline__ void put_pair4(const P& p, int m, int n, const i32x4& gate, const i32x4& up, const Ahead& a) {
+  const int left = p.N - n;
   float v[4];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int k = c < left ? n + c : n;
-    v[c] = gelu(value(gate[c], sa, p.sw[k], 0.f)) * value(up[c], sa, p.sw2[k], 0.f);
-  }
+  for (int c = 0; c < 4; ++c) v[c] = gelu(value(gate[c], a.sa, a.sw[c], 0.f)) * value(up[c], a.sa, a.more[c], 0.f);
   bf16_t* out = (bf16_t*)p.out + (size_t)m * p.ldc + n;
-  if (left == 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+  if (left >= 4) *(uint2*)out = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
   else
     for (int c = 0; c < left; ++c) out[c] = bf(v[c]);
 }
@@ -351,8 +371,10 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
     };
     auto row_scale = [&](int m) { return P.sa[m < M ? m : M - 1]; };
     auto load_cols = [&](const float* p, int n0, int n_end, float (&v)[8]) {
+      const f32x4 lo = p && n0 < n_end ? load4(p + n0, n_end - n0) : f32x4{0.f, 0.f, 0.f, 0.f};
+      const f32x4 hi = p && n0 + 4 < n_end ? load4(p + n0 + 4, n_end - n0 - 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < 8; ++c) v[c] = p && n0 + c < n_end ? p[n0 + c] : 0.f;
+      for (int c = 0; c < 4; ++c) { v[c] = lo[c]; v[4 + c] = hi[c]; }
     };
     float sa[RT];
     auto load_sa = [&]() {
@@ -503,18 +525,27 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       const int fr = ln >> 2, fc = ln & 3;               // my column (and the one 16 on) and piece when a unit is read back
       auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
       const uint32_t voff = (uint32_t)(fr * ldvt + fc * 8) * 2u;
+      float sr[RT / 2][8];                               // (all units' row scales, and where their first and last rows go, ahead of the stores)
+      int first[RT / 2], last[RT / 2];
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
         const int mb = mw + i * 32;
-        float s8[8];
+        first[i] = map[mb < M ? mb : M - 1];
+        last[i] = map[mb + 31 < M ? mb + 31 : M - 1];
+        if (mb + 32 <= M) {
+          const f32x4 lo = *(const f32x4_any*)(P.sa + mb + kq * 8), hi = *(const f32x4_any*)(P.sa + mb + kq * 8 + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s8[e] = row_scale(mb + kq * 8 + e);
-        bool consec = mb + 32 <= M;
-        int cb = 0;
-        if (consec) {
-          cb = map[mb];
-          consec = map[mb + 31] == cb + 31;
+          for (int e = 0; e < 4; ++e) { sr[i][e] = lo[e]; sr[i][4 + e] = hi[e]; }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sr[i][e] = row_scale(mb + kq * 8 + e);
         }
+      }
+#pragma unroll
+      for (int i = 0; i < RT / 2; ++i) {
+        const int mb = mw + i * 32, cb = first[i];
+        const float (&s8)[8] = sr[i];
+        const bool consec = mb + 32 <= M && last[i] == cb + 31;
         int col[8];
         if (!consec) {
 #pragma unroll
@@ -666,10 +697,15 @@ __global__ __launch_bounds__(256) void reduce_i8_kernel(const GemmI8 P) {
     for (int k = 1; k < P.splits; ++k) s += p[(size_t)k * CHUNK];
     return s;
   };
-  const i32x4 s = sum(c);
-  if (pair) put_pair4(P, m, n, s, sum(c + 2));
-  else if (vt) put_col4(P, m, n, s);
-  else put_row4(P, m, n, s);
+  if (pair) {
+    const Ahead a = fetch4<true>(P, m, n);
+    put_pair4(P, m, n, sum(c), sum(c + 2), a);
+  } else if (vt) {
+    put_col4(P, m, n, sum(c));
+  } else {
+    const Ahead a = fetch4<false>(P, m, n);
+    put_row4(P, m, n, sum(c), a);
+  }
 }
 
 // ---- few rows: the weights as a stream ---------------------------------------------------------------------------------
@@ -815,14 +851,33 @@ __global__ __launch_bounds__((StreamShape<MT, NT, PAIR>::WV * 64)) void stream_i
     for (int i = 0; i < IP; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) red[wave * (IP * NT * 64) + place(i, j, l16, kq)] = acc[i0 + i][j];
+    // up to four of a thread's results at a time: what the first ones need comes in while the sums are gathered
+    constexpr int ALL = IP * NC * 64, STEP = WV * 64, U = MT * NT >= 48 || ALL < 4 * STEP ? 2 : 4;
+    Ahead ahead[U];
+    int row[U], g[U];
+    bool in[U];
+    auto fetch = [&](int q0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int q = q0 + u * STEP;
+        row[u] = by_rows ? q % (IP * 16) : q / (NC * 4); g[u] = by_rows ? q / (IP * 16) : q % (NC * 4);
+        in[u] = q < ALL && m0 + i0 * 16 + row[u] < P.M && n0 + g[u] * 4 < P.N;
+        if (in[u]) ahead[u] = fetch4<PAIR>(P, m0 + i0 * 16 + row[u], n0 + g[u] * 4);
+      }
+    };
+    fetch(tid);
     __syncthreads();
-    for (int q = tid; q < IP * NC * 64; q += WV * 64) {
-      const int row = by_rows ? q % (IP * 16) : q / (NC * 4), g = by_rows ? q / (IP * 16) : q % (NC * 4);
-      const int m = m0 + i0 * 16 + row, n = n0 + g * 4;
-      if (m >= P.M || n >= P.N) continue;
-      const int i = row >> 4, j = g >> 2;
-      if constexpr (PAIR) put_pair4(P, m, n, sum(place(i, j, row & 15, g & 3)), sum(place(i, j + NC, row & 15, g & 3)));
-      else put_row4(P, m, n, sum(place(i, j, row & 15, g & 3)));
+    for (int q0 = tid;;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!in[u]) continue;
+        const int i = row[u] >> 4, j = g[u] >> 2, m = m0 + i0 * 16 + row[u], n = n0 + g[u] * 4;
+        if constexpr (PAIR) put_pair4(P, m, n, sum(place(i, j, row[u] & 15, g[u] & 3)), sum(place(i, j + NC, row[u] & 15, g[u] & 3)), ahead[u]);
+        else put_row4(P, m, n, sum(place(i, j, row[u] & 15, g[u] & 3)), ahead[u]);
+      }
+      q0 += U * STEP;
+      if (q0 >= ALL) break;
+      fetch(q0);
     }
   }
 }
