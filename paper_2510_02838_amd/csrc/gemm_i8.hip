@@ -201,9 +201,11 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
     t_step = (G >> 3) + (x < (G & 7) ? 1 : 0);
   }
   auto unit = [&](int t, int& tm, int& tn, int& k0, int& k1) {
-    const int u = t_first + t, tile = u / splits, sh = u - tile * splits, nk = P.K / 128;
+    const int u = t_first + t, tile = u / splits, sh = u - tile * splits, nk = P.K / 128;     // (sh * nk < 2^16: 8 shares, 2^10 slabs)
     tile_coords(P, tile, tm, tn);
-    k0 = (int)((long long)sh * nk / splits); k1 = (int)((long long)(sh + 1) * nk / splits);
+    // (scalar by hand: divided in vector registers, as an offset of the loads they would cost a loop around each of them)
+    tm = __builtin_amdgcn_readfirstlane(tm); tn = __builtin_amdgcn_readfirstlane(tn);
+    k0 = __builtin_amdgcn_readfirstlane(sh * nk / splits); k1 = __builtin_amdgcn_readfirstlane((sh + 1) * nk / splits);
   };
 
   // ---- the stream of slabs: one load of a wave fills 8 slab rows -------------------------------------------------------
@@ -508,8 +510,8 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       }
     };
     // Transposed columns: acc[2 i][c], acc[2 i + 1][c] hold rows 32 i + 8 kq + 0..7 of column 16 c + l16.  Units of 32 rows x 32
-    // columns; a lane writes 8 rows of a column as one 16-byte piece (at any 2-byte offset) when the 32 rows are neighbours
-    // in the transposed matrix, else in pairs and single elements.
+    // columns; a lane writes 8 rows of a column as one 16-byte piece (at any 2-byte offset: 1137 x 4096 x 4096 takes the same with every
+    // start) where these are neighbours in the transposed matrix, else in pairs and single elements.
     auto transposed = [&]() {
       typedef u32x4 u32x4_any __attribute__((aligned(2)));
       const int nv0 = nw - P.vt_from, ldvt = P.ldvt;
@@ -524,14 +526,15 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       }
       const int fr = ln >> 2, fc = ln & 3;               // my column (and the one 16 on) and piece when a unit is read back
       auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
-      const uint32_t voff = (uint32_t)(fr * ldvt + fc * 8) * 2u;
-      float sr[RT / 2][8];                               // (all units' row scales, and where their first and last rows go, ahead of the stores)
-      int first[RT / 2], last[RT / 2];
+      // All units' row scales and the columns of my pieces' rows, ahead of the stores: a load behind them waits for them to be done (pieces
+      // fetched one by one where they are stored made ragged rows cost 9 us more than neighbours, so 2).
+      float sr[RT / 2][8];
+      int col[RT / 2][8];
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
-        const int mb = mw + i * 32;
-        first[i] = map[mb < M ? mb : M - 1];
-        last[i] = map[mb + 31 < M ? mb + 31 : M - 1];
+        const int mb = mw + i * 32, mp = mb + fc * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) col[i][e] = map[mp + e < M ? mp + e : M - 1];
         if (mb + 32 <= M) {
           const f32x4 lo = *(const f32x4_any*)(P.sa + mb + kq * 8), hi = *(const f32x4_any*)(P.sa + mb + kq * 8 + 4);
 #pragma unroll
@@ -543,15 +546,8 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       }
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
-        const int mb = mw + i * 32, cb = first[i];
-        const float (&s8)[8] = sr[i];
-        const bool consec = mb + 32 <= M && last[i] == cb + 31;
-        int col[8];
-        if (!consec) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) col[e] = mb + fc * 8 + e < M ? map[mb + fc * 8 + e] : -1;
-          asm volatile("" :: "v"(col[0]), "v"(col[1]), "v"(col[2]), "v"(col[3]), "v"(col[4]), "v"(col[5]), "v"(col[6]), "v"(col[7]));
-        }
+        const int mp = mw + i * 32 + fc * 8;
+        const bool whole = mp + 8 <= M && col[i][7] == col[i][0] + 7;    // (columns rise)
 #pragma unroll
         for (int cp = 0; cp < 2; ++cp) {
 #pragma unroll
@@ -559,7 +555,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
             const int c = cp * 2 + q;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = value(acc[2 * i + (e >> 2)][c][e & 3], s8[e], sw[c], bv[c]);
+            for (int e = 0; e < 8; ++e) v[e] = value(acc[2 * i + (e >> 2)][c][e & 3], sr[i][e], sw[c], bv[c]);
             const u32x4 w = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
             *(u32x4*)at(q * 16 + l16, kq) = w;
           }
@@ -570,19 +566,14 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
           asm volatile("" ::: "memory");
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int f = cp * 32 + h * 16;
-            if (fr >= N - nw - f) continue;
-            if (consec) *(u32x4_any*)((char*)(vt_out + (size_t)(nv0 + f) * ldvt + cb) + voff) = w[h];
+            const int f = cp * 32 + h * 16 + fr;
+            if (f >= N - nw) continue;
+            bf16_t* const dst = vt_out + (size_t)(nv0 + f) * ldvt;
+            if (whole) *(u32x4_any*)(dst + col[i][0]) = w[h];
             else {
-              bf16_t* dst = vt_out + (size_t)(nv0 + f + fr) * ldvt;
 #pragma unroll
-              for (int e = 0; e < 8; e += 2) {
-                if (col[e + 1] == col[e] + 1 && (col[e] & 1) == 0) *(uint32_t*)(dst + col[e]) = w[h][e >> 1];
-                else {
-                  if (col[e] >= 0) dst[col[e]] = (bf16_t)w[h][e >> 1];
-                  if (col[e + 1] >= 0) dst[col[e + 1]] = (bf16_t)(w[h][e >> 1] >> 16);
-                }
-              }
+              for (int e = 0; e < 8; ++e)
+                if (mp + e < M) dst[col[i][e]] = (bf16_t)(w[h][e >> 1] >> (16 * (e & 1)));
             }
           }
           __builtin_amdgcn_sched_barrier(0);
