@@ -44,9 +44,9 @@ dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* 
  * [N] or NULL; K a multiple of 128, at most DIT_I8_MAX_K; lda, ldw multiples of 16 below 2^22.  out_kind, out, ldc, gate, gate_stride and row_req
  * as for dit_op_gemm (0 bf16, 1 float32, 2 bf16 of tanh-GELU, 3 float32 out += gate * C); any code -128..127 is
  * taken.  The result does not depend on how the product is cut up: it is the same, bit for bit, alone or among other rows.
- * work: dev scratch for the shares of a product split along K, may be NULL (not split); dit_op_gemm_i8_work_bytes
- * says how much the library's choice uses, less makes fewer shares.  Its contents carry nothing between calls; calls that
- * may overlap need one each. */
+ * work: dev scratch for the shares of a product that is split along K between workgroups (dit_op_gemm_i8_work_bytes says how much the
+ * library's choice takes, for most sizes nothing); with NULL or less another tile is taken.  Its contents carry nothing between
+ * calls; calls that may overlap need one each. */
 dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_scale, const void* W, int ldw, const float* w_scale,
                           const float* bias, int M, int N, int K, int out_kind, void* out, int ldc, const float* gate,
                           int gate_stride, const int* row_req, void* work, size_t work_bytes);
@@ -62,8 +62,11 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
                                      const float* w_scale, const float* bias, int M, int N, int K, void* out, int ldo,
                                      const int* col, void* work, size_t work_bytes);
 
-/* Scratch of one such call (pair != 0: dit_op_gemm_i8_geglu); 0 where nothing is split or the arguments are refused. */
+/* Scratch that the library's choice for a product uses (pair != 0: dit_op_gemm_i8_geglu), and the tile that it takes given so much:
+ * 100 * row tiles + column tiles, of 16, of a workgroup whose waves share K, or rows * 1000 + columns of an 8-wave one, in `splits` (may
+ * be NULL) shares of K.  Host only; 0 and -1 for sizes that the products refuse. */
 size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair);
+int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* splits);
 
 /* ---- the Encode stage in 8 bits ------------------------------------------------------- */
 

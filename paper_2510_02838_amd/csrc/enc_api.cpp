@@ -227,8 +227,9 @@ void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector
   L.act = take(M * ff * 2);
   L.bias_L = (int)rup(L.base.L, 64);
   L.bias = take((size_t)g.n_heads * (2 * (size_t)L.bias_L - 1) * 4);
-  L.partial_bytes = std::max(std::max(gemm_i8_work_bytes((int)M, (int)(3 * inner), (int)d, false), gemm_i8_work_bytes((int)M, (int)d, (int)inner, false)),
-                             std::max(gemm_i8_work_bytes((int)M, (int)ff, (int)d, true), gemm_i8_work_bytes((int)M, (int)d, (int)ff, false)));
+  auto scratch = [&](size_t N, size_t K, bool pair) { L.partial_bytes = std::max(L.partial_bytes, gemm_i8_work_bytes((int)M, (int)N, (int)K, pair)); };
+  L.partial_bytes = 0;
+  scratch(3 * inner, d, false); scratch(d, inner, false); scratch(ff, d, true); scratch(d, ff, false);
   L.partial = take(L.partial_bytes);
   L.total = o;
 }

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
     t_step = (G >> 3) + (x < (G & 7) ? 1 : 0);
   }
   auto unit = [&](int t, int& tm, int& tn, int& k0, int& k1) {
-    const int u = t_first + t, tile = u / splits, sh = u - tile * splits, nk = P.K / 128;     // (sh * nk < 2^16: 8 shares, 2^10 slabs)
+    const int u = t_first + t, tile = u / splits, sh = u - tile * splits, nk = P.K / 128;     // (sh * nk < 2^13: 4 shares, 2^10 slabs)
     tile_coords(P, tile, tm, tn);
     // (scalar by hand: divided in vector registers, as an offset of the loads they would cost a loop around each of them)
     tm = __builtin_amdgcn_readfirstlane(tm); tn = __builtin_amdgcn_readfirstlane(tn);
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
   };
   uint32_t oa[LA], ob[LB];           // byte offsets of my lane's 16 codes of each load, from the tile's first row
   const int8_t *sA, *sW;
-  int ld_t = blockIdx.x >> 3, ks = 0, ks_n = 0;
+  int ld_t = blockIdx.x >> 3, ks = 0, ks_n = 0;      // unit (in my XCD's range) and slab that are fetched next, and the end of its slabs
   auto aim = [&](int t) {
     int tm, tn;
     unit(t, tm, tn, ks, ks_n);
@@ -909,8 +909,7 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
     switch (nt) {
       case 2: launch_stream_t<MT, 2, true>(s, p); return true;
       case 4: launch_stream_t<MT, 4, true>(s, p); return true;
-      case 6: launch_stream_t<MT, 6, true>(s, p); return true;
-      case 8: if constexpr (MT >= 4 && MT <= 8) { launch_stream_t<MT, 8, true>(s, p); return true; }
+      case 6: if constexpr (MT <= 5) { launch_stream_t<MT, 6, true>(s, p); return true; }
     }
     return false;
   }
@@ -919,95 +918,89 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
     case 2: launch_stream_t<MT, 2, false>(s, p); return true;
     case 3: launch_stream_t<MT, 3, false>(s, p); return true;
     case 4: launch_stream_t<MT, 4, false>(s, p); return true;
-    case 6: if constexpr (MT >= 4) { launch_stream_t<MT, 6, false>(s, p); return true; }
-      return false;
-    case 8: if constexpr (MT >= 4 && MT <= 8) { launch_stream_t<MT, 8, false>(s, p); return true; }
-  }
-  return false;
-}
-bool launch_stream(hipStream_t s, GemmI8& p, int mt, int nt) {
-  p.splits = 1;
-  switch (mt) {
-    case 1: return launch_stream_m<1>(s, p, nt);
-    case 2: return launch_stream_m<2>(s, p, nt);
-    case 3: return launch_stream_m<3>(s, p, nt);
-    case 4: return launch_stream_m<4>(s, p, nt);
-    case 5: return launch_stream_m<5>(s, p, nt);
-    case 6: return launch_stream_m<6>(s, p, nt);
-    case 8: return launch_stream_m<8>(s, p, nt);
+    case 6: if constexpr (MT == 4 || MT == 5) { launch_stream_t<MT, 6, false>(s, p); return true; }
   }
   return false;
 }
 
 // ---- the choice of tile ----
-// Estimated time of a product in microseconds: the rounds of 256 workgroups, in each the slabs of one tile at a measured rate, and a fixed
-// part.  A slab of a stream tile takes what a CU pulls (85 GB/s) and a share of its products; of an 8-wave tile 0.5, 0.8 and 1.3 us
-// (1.42 where every CU has one and the clock falls).  Nothing is faster than its bytes at 4.8 TB/s.
-// Over 96 products of 1 to 4096 rows, 64 to 12288 columns and K from 256 to 10240, every candidate timed, the one chosen took 1.015 times the
-// best one's time in the mean and never more than 1.4 times.  What both sides take near the borders: 200 rows, N = 12288, K = 4096 stream
-// 23.8, 128x128 24.6; 333 rows 35.7 and 128x256 34.1; 1000 rows, N = 4096, K = 10240 stream 45.1, 128x128 54; 500 rows 31.8, 256x128 in four
-// shares 36; 128 rows, N = 4096, K = 4096 stream 7.6, 128x128 in four shares 16.9.
-struct Choice { int variant, splits; float us; };
-
+// The variant with the least estimated time, in microseconds: a start, the rounds of 256 workgroups, in each the slabs of one tile and a
+// fixed part (first loads, sums of the waves, epilogue).  A slab of a stream tile takes what a CU pulls, 2 KB a row tile at 85 GB/s, and a
+// share of its products; a slab of an 8-wave tile takes longer the more CUs run one (the clock falls with the matrix load: 256x256
+// tiles 0.75 us on 96 CUs, 1.2 on all).  Nothing is faster than its bytes at 4.8 TB/s.
+// The constants were fitted to 146 products of 1 to 6000 rows, 300 to 12288 columns and K from 512 to 10240 with every variant timed: the
+// one chosen took 1.007 times the best one's time in the mean, 1.06 at most.  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
+// 7.6, 128x128 14; 200 rows, N = 12288 stream 23.0, 128x128 20; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
+// 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Products split along K between
+// workgroups, with their sums through memory and a second launch, were at most 5 % faster, for 7 of 6000 drawn shapes, and are not built.
+struct Choice { int variant, splits; };
 Choice choose(int M, int N, int K, bool pair, size_t scratch) {
   const int nk = K / 128;
   const long long cols = pair ? 2LL * N : N;
-  const float least = 3.5f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
-  Choice best = {0, 1, 1e30f};
+  const float least = 3.8f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
+  Choice best = {0, 1};
+  float best_us = 0.f;
   auto offer = [&](int variant, int splits, float us) {
     if (us < least) us = least + us * 1e-3f;
-    if (us < best.us) best = Choice{variant, splits, us};
+    if (!best.variant || us < best_us) { best = Choice{variant, splits}; best_us = us; }
   };
-  for (int mt : {1, 2, 3, 4, 5, 6, 8})
-    for (int nt : {1, 2, 3, 4, 6, 8}) {
-      if ((pair && nt % 2) || (nt > 4 && mt < 4 && !(pair && nt == 6))) continue;
-      const long long wgs = (long long)((M + 16 * mt - 1) / (16 * mt)) * ((cols + 16 * nt - 1) / (16 * nt));
-      const long long rounds = (wgs + 255) / 256;
-      offer(100 * mt + nt, 1, 2.5f + (float)rounds * (nk * (0.0241f * (mt + nt) + 0.0022f * mt * nt) + (rounds > 1 ? 4.f : 2.f) + 0.03f * mt * nt));
+  for (int mt = 1; mt <= 6; ++mt)
+    for (int nt : {1, 2, 3, 4, 6}) {
+      if ((pair ? nt % 2 != 0 : nt == 6 && mt < 4) || (nt == 6 && mt == 6)) continue;      // (not built)
+      const long long wgs = (long long)((M + 16 * mt - 1) / (16 * mt)) * ((cols + 16 * nt - 1) / (16 * nt)), rounds = (wgs + 255) / 256;
+      offer(100 * mt + nt, 1, 2.8f + (float)rounds * (nk * (0.0242f * (mt + nt) + 0.0027f * mt * nt) + (rounds > 1 ? 4.3f : 2.f) + 0.03f * mt * nt));
     }
-  const struct { int bm, bn; float slab, full, fixed; } tiles[] = {{128, 128, 0.5f, 0.5f, 6.5f}, {128, 256, 0.8f, 0.86f, 7.f},
-                                                                  {256, 128, 0.8f, 0.86f, 7.f}, {256, 256, 1.28f, 1.42f, 8.f}};
+  const struct { int bm, bn; float few, many, fixed; } tiles[] = {{128, 128, 0.285f, 0.468f, 3.5f}, {128, 256, 0.536f, 0.701f, 5.8f},
+                                                                  {256, 128, 0.536f, 0.701f, 5.8f}, {256, 256, 0.65f, 1.185f, 11.5f}};
   for (const auto& t : tiles) {
     const long long n = (long long)((M + t.bm - 1) / t.bm) * ((cols + t.bn - 1) / t.bn);
-    offer(t.bm * 1000 + t.bn, 1, 3.f + (float)((n + 255) / 256) * (nk * (n >= 256 ? t.full : t.slab) + t.fixed));
-    // shares of K: one round of them, their sums through memory and a second launch
-    for (int s = 2; s <= 8 && n * s <= 256 && nk / s >= 8; ++s)
-      if ((size_t)n * s * t.bm * t.bn * 4 <= scratch)
-        offer(t.bm * 1000 + t.bn, s, 12.f + (nk + s - 1) / s * t.slab + t.fixed * 0.7f + (float)n * s * t.bm * t.bn / 1e6f);
+    const float load = n < 410 ? (float)n / 410.f : 1.f;
+    offer(t.bm * 1000 + t.bn, 1, 2.4f + (float)((n + 255) / 256) * (nk * (t.few + (t.many - t.few) * load) + t.fixed));
   }
+  // Shares of K of 128x128 tiles, where these leave CUs empty: their sums go through memory to a second launch.
+  const long long n = (long long)((M + 127) / 128) * ((cols + 127) / 128);
+  for (int s = 2; s <= 4 && n * s <= 256 && nk >= 8 * s; ++s)
+    if ((size_t)n * s * (128 * 128 * 4) <= scratch)
+      offer(128128, s, 9.6f + (float)((nk + s - 1) / s) * (0.285f + 0.183f * (float)(n * s) / 410.f) + 2.5f + (float)n * s * 0.0164f);
   return best;
 }
 
 }  // namespace
 
-size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {
-  const Choice c = choose(M, N, K, pair, ~(size_t)0);
-  if (c.splits == 1) return 0;
-  const int bm = c.variant / 1000, bn = c.variant % 1000;
-  return (size_t)((M + bm - 1) / bm) * (((pair ? 2LL * N : N) + bn - 1) / bn) * c.splits * bm * bn * 4;
+// variant 100 MT + NT: a stream tile; BM*1000 + BN: an 8-wave tile, 128x128 ones with p.splits shares of K
+bool launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant) {
+  if (variant != 128128) p.splits = 1;
+  switch (variant) {
+    case 256256: launch8<256, 256, 2, 4, 2>(s, p); return true;
+    case 256128: launch8<256, 128, 4, 2, 3>(s, p); return true;
+    case 128256: launch8<128, 256, 2, 4, 3>(s, p); return true;
+    case 128128: launch8<128, 128, 4, 2, 4>(s, p); return true;
+  }
+  switch (variant / 100) {
+    case 1: return launch_stream_m<1>(s, p, variant % 100);
+    case 2: return launch_stream_m<2>(s, p, variant % 100);
+    case 3: return launch_stream_m<3>(s, p, variant % 100);
+    case 4: return launch_stream_m<4>(s, p, variant % 100);
+    case 5: return launch_stream_m<5>(s, p, variant % 100);
+    case 6: return launch_stream_m<6>(s, p, variant % 100);
+  }
+  return false;
 }
 
-// variant 100 MT + NT: a stream tile; BM*1000 + BN: an 8-wave tile with p.splits shares
-int launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant) {
-  if (variant < 1000) return launch_stream(s, p, variant / 100, variant % 100) ? variant : -1;
-  if (variant == 256256) launch8<256, 256, 2, 4, 2>(s, p);
-  else if (variant == 256128) launch8<256, 128, 4, 2, 3>(s, p);
-  else if (variant == 128256) launch8<128, 256, 2, 4, 3>(s, p);
-  else if (variant == 128128) launch8<128, 128, 4, 2, 4>(s, p);
-  else return -1;
-  return variant;
+int gemm_i8_variant(int M, int N, int K, bool pair, size_t scratch, int* splits) {
+  const Choice c = choose(M, N, K, pair, scratch);
+  *splits = c.splits;
+  return c.variant;
+}
+size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {
+  const Choice c = choose(M, N, K, pair, ~(size_t)0);
+  return c.splits == 1 ? 0 : (size_t)((M + 127) / 128) * (((pair ? 2LL * N : N) + 127) / 128) * c.splits * (128 * 128 * 4);
 }
 
 void launch_gemm_i8(hipStream_t s, GemmI8& p) {
   const Choice c = choose(p.M, p.N, p.K, p.W2 != nullptr, p.partial ? p.partial_bytes : 0);
   p.splits = c.splits;
   launch_gemm_i8_variant(s, p, c.variant);
-}
-
-int gemm_i8_choice(int M, int N, int K, bool pair, size_t scratch, int* splits) {
-  const Choice c = choose(M, N, K, pair, scratch);
-  *splits = c.splits;
-  return c.variant;
 }
 
 }  // namespace dit

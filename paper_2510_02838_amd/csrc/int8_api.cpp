@@ -101,9 +101,16 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
   return launched();
 }
 
-size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair) {
-  if (M <= 0 || N <= 0 || K <= 0 || K % 128 || K > DIT_I8_MAX_K || !countable(M, N)) return 0;
-  return gemm_i8_work_bytes(M, N, K, pair != 0);
+static bool sizes_ok(int M, int N, int K) { return M > 0 && N > 0 && K > 0 && K % 128 == 0 && K <= DIT_I8_MAX_K && countable(M, N); }
+
+size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair) { return sizes_ok(M, N, K) ? gemm_i8_work_bytes(M, N, K, pair != 0) : 0; }
+
+int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* splits) {
+  if (!sizes_ok(M, N, K)) return -1;
+  int s = 1;
+  const int tile = gemm_i8_variant(M, N, K, pair != 0, work_bytes, &s);
+  if (splits) *splits = s;
+  return tile;
 }
 
 }  // extern "C"

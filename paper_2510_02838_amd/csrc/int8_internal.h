@@ -21,12 +21,13 @@ struct GemmI8 {
   void* out; int ldc;
   const float* gate; int gate_stride; const int* row_req;
   bf16_t* vt; int ldvt; const int* vt_col; int vt_from;
+  int* partial; size_t partial_bytes; // scratch for the sums of a product split along K, or null
   int tiles_m, tiles_n, splits;       // filled by the launcher
-  int* partial;                       // scratch for the shares of K, or null
-  size_t partial_bytes;
 };
 void launch_gemm_i8(hipStream_t s, GemmI8& p);
-int launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant);
-size_t gemm_i8_work_bytes(int M, int N, int K, bool pair);
+size_t gemm_i8_work_bytes(int M, int N, int K, bool pair);      // scratch of its choice
+// its choice of tile with so much scratch (host only), and a launch with a given one (false: no such variant)
+int gemm_i8_variant(int M, int N, int K, bool pair, size_t scratch, int* splits);
+bool launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant);
 
 }  // namespace dit

@@ -17,6 +17,7 @@ _SIGS = {
     "dit_op_gemm_i8_geglu": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _i, _vp, _sz]),
     "dit_op_gemm_i8_transposed": (_i, [_vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _vp, _i, _vp, _vp, _sz]),
     "dit_op_gemm_i8_work_bytes": (_sz, [_i, _i, _i, _i]),
+    "dit_op_gemm_i8_tile": (_i, [_i, _i, _i, _i, _sz, _ip]),
     "enc_i8_weight_bytes": (_sz, [_vp]),
     "enc_i8_workspace_bytes": (_sz, [_vp, _i, _ip]),
     "enc_i8_quantize": (_i, [_vp, _vp, _sz]),

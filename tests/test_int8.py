@@ -68,7 +68,14 @@ def test_products_check_their_arguments(Q):
     assert plain(M=0) == plain(N=0) == pair(M=0) == tr(M=0) == 0
     assert pair(up=None) == pair(us=None) == 1 and pair(up=264) == pair(ld=112) == pair(ldc=12) == pair(ldc=0) == 2
     assert tr(col=None) == 1 and tr(ldo=0) == tr(ldo=12) == tr(out=264) == 2
-    assert Q.dit_op_gemm_i8_work_bytes(0, 8, 128, 0) == Q.dit_op_gemm_i8_work_bytes(4, 8, 100, 0) == Q.dit_op_gemm_i8_work_bytes(4, 8, 131072, 0) == 0
+    for sizes in ((0, 8, 128), (4, 0, 128), (4, 8, 100), (4, 8, 131072), (1 << 30, 1 << 30, 128)):
+        assert Q.dit_op_gemm_i8_tile(*sizes, 0, 0, None) == -1 and Q.dit_op_gemm_i8_work_bytes(*sizes, 0) == 0
+    # four by thirty-two tiles of 128x128 in two shares of 64 KB each, with as much scratch; without, no shares
+    n, s = Q.C.c_int(), 4 * 32 * 2 * 65536
+    assert Q.dit_op_gemm_i8_work_bytes(500, 4096, 10240, 0) == s
+    assert Q.dit_op_gemm_i8_tile(500, 4096, 10240, 0, s, n) == 128128 and n.value == 2
+    Q.dit_op_gemm_i8_tile(500, 4096, 10240, 0, s - 1, n)
+    assert n.value == 1
     with pytest.raises(Exception, match="DIT_ESHAPE"):
         Q.check(2)
 
@@ -274,11 +281,31 @@ def gelu_bound(v, dv):
 SHAPES = [(1, 1, 128), (1, 256, 128), (2, 17, 256), (1, 4096, 4096), (7, 100, 1280), (16, 512, 384), (17, 520, 2048), (31, 64, 10240), (32, 1536, 1536), (33, 1000, 512),
           (48, 768, 4096), (63, 130, 640), (64, 4096, 512), (65, 333, 1152), (77, 2048, 4096), (96, 250, 256), (127, 384, 10240), (128, 1280, 1280), (129, 1536, 128),
           (200, 4096, 1024), (255, 257, 768), (256, 256, 4096), (300, 5120, 256), (333, 1000, 1536), (500, 4096, 2560), (640, 640, 384), (1000, 1537, 512), (1137, 4096, 256),
-          (2049, 1100, 256), (4100, 2304, 128)]
+          (2049, 1100, 256), (4100, 2304, 128), (500, 4096, 5120), (130, 1300, 10240), (250, 6000, 9600)]
+
+# the least work that takes each of the tiles (tile: sizes)
+TILES = {101: (3, 5, 128), 102: (1, 4152, 128), 103: (2, 9022, 128), 104: (1, 13146, 128), 201: (4450, 1, 128), 202: (17, 6818, 128), 203: (17, 10516, 128),
+         204: (19, 13936, 768), 301: (9774, 1, 128), 302: (11428, 1, 896), 303: (10878, 34, 128), 304: (33, 12767, 128), 401: (12640, 1, 128),
+         402: (12597, 20, 128), 403: (13502, 34, 128), 404: (105, 6709, 128), 406: (1, 17713, 128), 501: (19569, 1, 128), 502: (17046, 1, 640),
+         503: (8330, 71, 128), 504: (65, 12660, 128), 506: (14264, 1, 7296), 601: (3240, 101, 128), 602: (15604, 4, 896), 603: (82, 9537, 128),
+         604: (11375, 104, 128), 128128: (1, 26313, 128), 128256: (5, 39579, 128), 256128: (132, 20313, 128), 256256: (132, 38639, 256)}
+PAIRS = {102: (3, 5, 128), 104: (1, 4152, 128), 106: (1, 9022, 128), 202: (4450, 1, 128), 204: (17, 6818, 128), 206: (17, 10516, 128), 302: (9774, 1, 128),
+         304: (38, 4463, 128), 306: (10878, 34, 128), 402: (12640, 1, 128), 404: (12597, 20, 128), 406: (13502, 34, 128), 502: (19569, 1, 128),
+         504: (18936, 17, 128), 506: (8330, 71, 128), 602: (3240, 101, 128), 604: (10646, 50, 128), 128128: (1, 13146, 128), 128256: (2, 17713, 128),
+         256128: (131, 11066, 128), 256256: (131, 27190, 128)}
+
+
+def test_every_tile_is_tested(Q):
+    """The lists above reach what they say, and no drawn shape takes a tile that they leave out."""
+    for pair, table in ((0, TILES), (1, PAIRS)):
+        assert {t: Q.dit_op_gemm_i8_tile(*s, pair, 0, None) for t, s in table.items()} == {t: t for t in table}
+        rng = np.random.RandomState(pair)
+        for M, N, K in zip(*(np.exp(rng.uniform(0, math.log(m), 3000)).astype(int) for m in (20000, 40000, 160))):
+            assert Q.dit_op_gemm_i8_tile(int(M), int(N), 128 * int(K), pair, 0, None) in table
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("M,N,K", SHAPES + list(TILES.values()))
 def test_product_of_codes_in_every_form(torch, Q, M, N, K):
     P = Product(torch, M, N, K, seed=M + N + K, pad_a=48, pad_w=16)
     p, b = P.exact(), P.bias.double()
@@ -309,7 +336,7 @@ def test_product_of_codes_in_every_form(torch, Q, M, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("M,N,K", SHAPES + list(PAIRS.values()))
 def test_gated_pair_of_codes(torch, Q, M, N, K):
     P = Product(torch, M, N, K, seed=M + N + K, pad_a=16, pad_w=32, pair=True)
     g, u = P.exact(), P.exact(P.W2, P.sw2)
