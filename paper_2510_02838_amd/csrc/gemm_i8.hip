@@ -925,19 +925,19 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
 
 // ---- the choice of tile ----
 // The variant with the least estimated time, in microseconds: a start, the rounds of 256 workgroups, in each the slabs of one tile and a
-// fixed part (first loads, sums of the waves, epilogue).  A slab of a stream tile takes what a CU pulls, 2 KB a row tile at 85 GB/s, and a
-// share of its products; a slab of an 8-wave tile takes longer the more CUs run one (the clock falls with the matrix load: 256x256
-// tiles 0.75 us on 96 CUs, 1.2 on all).  Nothing is faster than its bytes at 4.8 TB/s.
-// The constants were fitted to 146 products of 1 to 6000 rows, 300 to 12288 columns and K from 512 to 10240 with every variant timed: the
-// one chosen took 1.007 times the best one's time in the mean, 1.06 at most.  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
-// 7.6, 128x128 14; 200 rows, N = 12288 stream 23.0, 128x128 20; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
-// 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Products split along K between
-// workgroups, with their sums through memory and a second launch, were at most 5 % faster, for 7 of 6000 drawn shapes, and are not built.
+// fixed part (first loads, sums of the waves, epilogue).  A slab of a stream tile takes 2 KB a row tile of what a CU pulls and a share of
+// its products; a slab of an 8-wave tile takes longer the more CUs run one (the clock falls with the matrix load: 256x256 0.7 us for
+// one, 1.2 with all of them busy, 1.3 round after round).  Nothing is faster than its bytes at 4.8 TB/s.
+// The constants were fitted to 312 products of 1 to 8000 rows, 300 to 12288 columns and K from 512 to 10240 with every variant timed: the
+// one chosen took 1.005 times the best one's time in the mean, 1.07 at most.  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
+// 7.6, 128x128 14; 200 rows, N = 12288 128x128 20, stream 23; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
+// 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Two shares of K: 500 rows, N = 4096,
+// K = 10240 30.7, unsplit 36, stream 34; 248 rows, N = 6176, K = 9600 27 % less than anything unsplit.
 struct Choice { int variant, splits; };
 Choice choose(int M, int N, int K, bool pair, size_t scratch) {
   const int nk = K / 128;
   const long long cols = pair ? 2LL * N : N;
-  const float least = 3.8f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
+  const float least = 0.4f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
   Choice best = {0, 1};
   float best_us = 0.f;
   auto offer = [&](int variant, int splits, float us) {
@@ -948,20 +948,21 @@ Choice choose(int M, int N, int K, bool pair, size_t scratch) {
     for (int nt : {1, 2, 3, 4, 6}) {
       if ((pair ? nt % 2 != 0 : nt == 6 && mt < 4) || (nt == 6 && mt == 6)) continue;      // (not built)
       const long long wgs = (long long)((M + 16 * mt - 1) / (16 * mt)) * ((cols + 16 * nt - 1) / (16 * nt)), rounds = (wgs + 255) / 256;
-      offer(100 * mt + nt, 1, 2.8f + (float)rounds * (nk * (0.0242f * (mt + nt) + 0.0027f * mt * nt) + (rounds > 1 ? 4.3f : 2.f) + 0.03f * mt * nt));
+      offer(100 * mt + nt, 1, 0.6f + (float)rounds * (nk * (0.0141f * (mt + nt) + 0.005f * mt * nt) + (rounds > 1 ? 1.95f : 2.9f) + 0.054f * mt * nt));
     }
-  const struct { int bm, bn; float few, many, fixed; } tiles[] = {{128, 128, 0.285f, 0.468f, 3.5f}, {128, 256, 0.536f, 0.701f, 5.8f},
-                                                                  {256, 128, 0.536f, 0.701f, 5.8f}, {256, 256, 0.65f, 1.185f, 11.5f}};
-  for (const auto& t : tiles) {
-    const long long n = (long long)((M + t.bm - 1) / t.bm) * ((cols + t.bn - 1) / t.bn);
-    const float load = n < 410 ? (float)n / 410.f : 1.f;
-    offer(t.bm * 1000 + t.bn, 1, 2.4f + (float)((n + 255) / 256) * (nk * (t.few + (t.many - t.few) * load) + t.fixed));
+  struct Tile { int bm, bn; float one, all, on, fixed; };          // a slab of the only tile, of 256 tiles, of round after round
+  static constexpr Tile tiles[] = {{128, 128, 0.305f, 0.458f, 0.477f, 3.3f}, {128, 256, 0.43f, 0.70f, 0.75f, 5.7f},
+                                   {256, 128, 0.43f, 0.70f, 0.75f, 5.7f}, {256, 256, 0.70f, 1.19f, 1.29f, 9.6f}};
+  auto slab = [](const Tile& t, long long n) { return t.one + (t.all - t.one) * (float)n / 256.f; };
+  for (const Tile& t : tiles) {
+    const long long n = (long long)((M + t.bm - 1) / t.bm) * ((cols + t.bn - 1) / t.bn), full = n > 256 ? n / 256 : 0, rest = n - full * 256;
+    offer(t.bm * 1000 + t.bn, 1, 2.6f + (float)full * (nk * t.on + t.fixed) + (rest ? nk * slab(t, rest) + t.fixed : 0.f));
   }
   // Shares of K of 128x128 tiles, where these leave CUs empty: their sums go through memory to a second launch.
   const long long n = (long long)((M + 127) / 128) * ((cols + 127) / 128);
   for (int s = 2; s <= 4 && n * s <= 256 && nk >= 8 * s; ++s)
     if ((size_t)n * s * (128 * 128 * 4) <= scratch)
-      offer(128128, s, 9.6f + (float)((nk + s - 1) / s) * (0.285f + 0.183f * (float)(n * s) / 410.f) + 2.5f + (float)n * s * 0.0164f);
+      offer(128128, s, 5.3f + (float)((nk + s - 1) / s) * slab(tiles[0], n * s) + 2.3f + (float)n * s * 0.018f);
   return best;
 }
 

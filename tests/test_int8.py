@@ -284,15 +284,16 @@ SHAPES = [(1, 1, 128), (1, 256, 128), (2, 17, 256), (1, 4096, 4096), (7, 100, 12
           (2049, 1100, 256), (4100, 2304, 128), (500, 4096, 5120), (130, 1300, 10240), (250, 6000, 9600)]
 
 # the least work that takes each of the tiles (tile: sizes)
-TILES = {101: (3, 5, 128), 102: (1, 4152, 128), 103: (2, 9022, 128), 104: (1, 13146, 128), 201: (4450, 1, 128), 202: (17, 6818, 128), 203: (17, 10516, 128),
-         204: (19, 13936, 768), 301: (9774, 1, 128), 302: (11428, 1, 896), 303: (10878, 34, 128), 304: (33, 12767, 128), 401: (12640, 1, 128),
-         402: (12597, 20, 128), 403: (13502, 34, 128), 404: (105, 6709, 128), 406: (1, 17713, 128), 501: (19569, 1, 128), 502: (17046, 1, 640),
-         503: (8330, 71, 128), 504: (65, 12660, 128), 506: (14264, 1, 7296), 601: (3240, 101, 128), 602: (15604, 4, 896), 603: (82, 9537, 128),
-         604: (11375, 104, 128), 128128: (1, 26313, 128), 128256: (5, 39579, 128), 256128: (132, 20313, 128), 256256: (132, 38639, 256)}
-PAIRS = {102: (3, 5, 128), 104: (1, 4152, 128), 106: (1, 9022, 128), 202: (4450, 1, 128), 204: (17, 6818, 128), 206: (17, 10516, 128), 302: (9774, 1, 128),
-         304: (38, 4463, 128), 306: (10878, 34, 128), 402: (12640, 1, 128), 404: (12597, 20, 128), 406: (13502, 34, 128), 502: (19569, 1, 128),
-         504: (18936, 17, 128), 506: (8330, 71, 128), 602: (3240, 101, 128), 604: (10646, 50, 128), 128128: (1, 13146, 128), 128256: (2, 17713, 128),
-         256128: (131, 11066, 128), 256256: (131, 27190, 128)}
+TILES = {101: (3, 5, 128), 102: (1, 4162, 128), 103: (1, 8338, 128), 104: (1, 12640, 128), 201: (4125, 1, 128), 202: (17, 6222, 128), 203:
+         (18, 10487, 128), 204: (18, 13030, 128), 301: (8416, 1, 128), 302: (10476, 19, 128), 303: (10082, 33, 128), 304: (38, 12298, 128),
+         401: (12374, 1, 128), 402: (13877, 17, 128), 403: (14781, 33, 128), 404: (50, 12921, 128), 406: (18, 16645, 128), 501: (16466, 1,
+         128), 502: (19992, 17, 128), 503: (16558, 33, 128), 504: (8921, 97, 128), 506: (132, 8917, 128), 601: (4156, 67, 128), 602: (15813,
+         2, 1920), 603: (88, 8513, 128), 604: (11110, 102, 128), 128128: (1, 21015, 4480), 128256: (82, 32929, 128), 256128: (176, 17220,
+         128), 256256: (130, 37535, 128)}
+PAIRS = {102: (3, 5, 128), 104: (1, 4128, 128), 106: (1, 8203, 128), 202: (4101, 1, 128), 204: (19, 6280, 128), 206: (17, 8669, 128), 302:
+         (8286, 1, 128), 304: (34, 4318, 128), 306: (8402, 38, 128), 402: (12381, 1, 128), 404: (15771, 17, 128), 406: (49, 8488, 128), 502:
+         (16480, 1, 128), 504: (19688, 17, 128), 506: (67, 8335, 128), 602: (3374, 97, 128), 604: (10372, 50, 128), 128128: (1, 10609,
+         4352), 128256: (38, 26248, 128), 256128: (162, 9909, 128), 256256: (137, 18938, 128)}
 
 
 def test_every_tile_is_tested(Q):
