@@ -24,6 +24,7 @@ extern "C" {
 
 enum { DIT_X_BF16 = 0, DIT_X_F32 = 1 };
 enum { DIT_I8_MAX_ROW = 16384, /* columns of a row that gets codes */
+       DIT_I8_MAX_ROWS = 1 << 23, /* rows of one such call */
        DIT_I8_MAX_K = 131072 - 128 /* K of a product: its sums stay inside 32 bits */ };
 
 /* Codes and scales of the rows of x [M][ldx], d columns each (1..DIT_I8_MAX_ROW, any number), x_kind DIT_X_*.

@@ -6,11 +6,12 @@ using namespace dit;
 
 namespace {
 inline bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
+inline bool off4(const void* p) { return ((uintptr_t)p & 3) != 0; }
 inline int rup128(int n) { return (n + 127) / 128 * 128; }
 inline dit_status launched() { return hipGetLastError() == hipSuccess ? DIT_OK : DIT_EDEVICE; }
 
 // (tiles and shares are counted in 32 bits)
-inline bool countable(int M, int N) { return (M + 127LL) / 128 * ((N + 15LL) / 16) < (1LL << 26); }
+inline bool countable(int M, int N) { return M <= (1 << 30) && N <= (1 << 30) && (M + 127LL) / 128 * ((N + 15LL) / 16) < (1LL << 26); }
 
 // what the three forms of the product have in common
 dit_status check_product(const void* A, int lda, const float* a_scale, const void* W, int ldw, const float* w_scale, int M, int N, int K,
@@ -19,7 +20,7 @@ dit_status check_product(const void* A, int lda, const float* a_scale, const voi
   if (M < 0 || N < 0 || K <= 0 || K % 128 || K > DIT_I8_MAX_K || lda < K || ldw < K || lda % 16 || ldw % 16) return DIT_ESHAPE;
   if (lda >= (1 << 22) || ldw >= (1 << 22)) return DIT_ESHAPE;                       // 32-bit offsets inside a tile
   if (!countable(M, N)) return DIT_ESHAPE;
-  if (off16(A) || off16(W) || off16(out) || off16(work)) return DIT_ESHAPE;
+  if (off16(A) || off16(W) || off16(out) || off16(work) || off4(a_scale) || off4(w_scale)) return DIT_ESHAPE;
   return DIT_OK;
 }
 
@@ -38,8 +39,8 @@ extern "C" {
 
 dit_status dit_op_quantize_i8(void* stream, const void* x, int x_kind, int ldx, int M, int d, void* codes, int ldq, float* scale) {
   if (!x || !codes || !scale || (x_kind != DIT_X_BF16 && x_kind != DIT_X_F32)) return DIT_EINVAL;
-  if (M < 0 || d < 1 || d > DIT_I8_MAX_ROW || ldx < d || ldx % (x_kind == DIT_X_F32 ? 4 : 8) || ldq < rup128(d) || ldq % 16) return DIT_ESHAPE;
-  if (off16(x) || off16(codes)) return DIT_ESHAPE;
+  if (M < 0 || M > DIT_I8_MAX_ROWS || d < 1 || d > DIT_I8_MAX_ROW || ldx < d || ldx % (x_kind == DIT_X_F32 ? 4 : 8) || ldq < rup128(d) || ldq % 16) return DIT_ESHAPE;
+  if (off16(x) || off16(codes) || off4(scale)) return DIT_ESHAPE;
   if (M == 0) return DIT_OK;
   launch_quantize_i8((hipStream_t)stream, x, x_kind == DIT_X_F32, ldx, M, d, (int8_t*)codes, ldq, scale);
   return launched();
@@ -50,10 +51,10 @@ dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* 
   if (!x || !gain || !codes || !scale) return DIT_EINVAL;
   if (delta && delta_kind != DIT_X_BF16 && delta_kind != DIT_X_F32) return DIT_EINVAL;
   if (!(eps > 0.f) || eps > 1e30f) return DIT_EINVAL;
-  if (M < 0 || d < 1 || d > DIT_I8_MAX_ROW || ldx < d || ldx % 4 || ldq < rup128(d) || ldq % 16) return DIT_ESHAPE;
+  if (M < 0 || M > DIT_I8_MAX_ROWS || d < 1 || d > DIT_I8_MAX_ROW || ldx < d || ldx % 4 || ldq < rup128(d) || ldq % 16) return DIT_ESHAPE;
   if (delta && (ldd < d || ldd % (delta_kind == DIT_X_F32 ? 4 : 8) || off16(delta))) return DIT_ESHAPE;
   if (x_out && (ldo < d || ldo % 4 || off16(x_out) || (x_out == x && ldo != ldx))) return DIT_ESHAPE;
-  if (off16(x) || off16(codes) || off16(gain)) return DIT_ESHAPE;
+  if (off16(x) || off16(codes) || off16(gain) || off4(scale)) return DIT_ESHAPE;
   if (M == 0) return DIT_OK;
   launch_rmsnorm_i8((hipStream_t)stream, x, ldx, delta, delta_kind == DIT_X_F32, ldd, gain, eps, M, d, x_out, ldo, (int8_t*)codes, ldq, scale);
   return launched();
@@ -65,7 +66,8 @@ dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_s
   const dit_status st = check_product(A, lda, a_scale, W, ldw, w_scale, M, N, K, out, work);
   if (st != DIT_OK) return st;
   if (out_kind < OUT_BF16 || out_kind > OUT_RESID_F32) return DIT_EINVAL;
-  if (ldc < N || ldc % (out_kind == OUT_F32 || out_kind == OUT_RESID_F32 ? 4 : 8)) return DIT_ESHAPE;
+  if (ldc < N || ldc % (out_kind == OUT_F32 || out_kind == OUT_RESID_F32 ? 4 : 8) || off4(bias)) return DIT_ESHAPE;
+  if (out_kind == OUT_RESID_F32 && (off4(gate) || off4(row_req))) return DIT_ESHAPE;
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W, ldw, w_scale, bias, M, N, K, out_kind, out, ldc, work, work_bytes);
   if (out_kind == OUT_RESID_F32) { p.gate = gate; p.gate_stride = gate_stride; p.row_req = row_req; }
@@ -79,7 +81,7 @@ dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const floa
   const dit_status st = check_product(A, lda, a_scale, W_gate, ldw, gate_scale, M, N, K, out, work);
   if (st != DIT_OK) return st;
   if (!W_up || !up_scale) return DIT_EINVAL;
-  if (ldc < N || ldc % 8 || off16(W_up)) return DIT_ESHAPE;
+  if (ldc < N || ldc % 8 || off16(W_up) || off4(up_scale)) return DIT_ESHAPE;
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W_gate, ldw, gate_scale, nullptr, M, N, K, OUT_BF16, out, ldc, work, work_bytes);
   p.W2 = (const int8_t*)W_up; p.sw2 = up_scale;
@@ -93,7 +95,7 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
   const dit_status st = check_product(A, lda, a_scale, W, ldw, w_scale, M, N, K, out, work);
   if (st != DIT_OK) return st;
   if (!col) return DIT_EINVAL;
-  if (ldo < M || ldo % 8) return DIT_ESHAPE;
+  if (ldo < M || ldo % 8 || off4(bias) || off4(col)) return DIT_ESHAPE;
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W, ldw, w_scale, bias, M, N, K, OUT_BF16, nullptr, 0, work, work_bytes);
   p.vt = (bf16_t*)out; p.ldvt = ldo; p.vt_col = col; p.vt_from = 0;

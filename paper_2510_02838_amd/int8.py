@@ -8,7 +8,7 @@ from .encoder import Encoder, _lens
 _vp, _i, _sz, _f, _ip = C.c_void_p, C.c_int, C.c_size_t, C.c_float, C.POINTER(C.c_int)
 
 X_BF16, X_F32 = 0, 1
-MAX_ROW, MAX_K = 16384, 131072 - 128
+MAX_ROW, MAX_ROWS, MAX_K = 16384, 1 << 23, 131072 - 128
 
 _SIGS = {
     "dit_op_quantize_i8": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _i, _vp]),

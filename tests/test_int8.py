@@ -44,14 +44,14 @@ def test_row_operators_check_their_arguments(Q):
     quant = lambda x=256, kind=0, ldx=128, M=4, d=100, codes=256, ldq=128, scale=256: Q.dit_op_quantize_i8(None, x, kind, ldx, M, d, codes, ldq, scale)  # noqa: E731
     assert quant(x=None) == quant(codes=None) == quant(scale=None) == quant(kind=2) == 1
     assert quant(M=-1) == quant(d=0) == quant(d=16385, ldx=16392, ldq=16512) == quant(ldx=96) == quant(ldx=100) == quant(ldq=112) == quant(ldq=136) == 2
-    assert quant(kind=1, ldx=102) == quant(x=264) == quant(codes=264) == 2
+    assert quant(kind=1, ldx=102) == quant(x=264) == quant(codes=264) == quant(scale=258) == quant(M=Q.MAX_ROWS + 1) == 2
     assert quant(M=0) == 0
     norm = lambda x=256, ldx=128, delta=256, dk=0, ldd=128, gain=256, eps=1e-6, M=4, d=100, xo=256, ldo=128, codes=256, ldq=128, scale=256: (  # noqa: E731
         Q.dit_op_rmsnorm_i8(None, x, ldx, delta, dk, ldd, gain, eps, M, d, xo, ldo, codes, ldq, scale))
     assert norm(x=None) == norm(gain=None) == norm(codes=None) == norm(scale=None) == norm(dk=5) == 1
     assert norm(eps=0.0) == norm(eps=-1.0) == norm(eps=math.nan) == norm(eps=math.inf) == 1
     assert norm(M=-1) == norm(d=0) == norm(d=16385, ldx=16388, ldd=16392, ldo=16388, ldq=16512) == norm(ldx=96) == norm(ldx=102) == norm(ldq=112) == 2
-    assert norm(ldd=96) == norm(ldd=100) == norm(delta=264) == norm(ldo=96) == norm(xo=264) == norm(ldo=132) == norm(x=264) == norm(gain=260) == 2
+    assert norm(ldd=96) == norm(ldd=100) == norm(delta=264) == norm(ldo=96) == norm(xo=264) == norm(ldo=132) == norm(x=264) == norm(gain=260) == norm(scale=257) == norm(M=Q.MAX_ROWS + 1) == 2
     assert norm(M=0) == norm(M=0, delta=None, dk=9, xo=None) == norm(M=0, xo=512, ldo=132) == 0
 
 
@@ -64,10 +64,10 @@ def test_products_check_their_arguments(Q):
     assert plain(A=None) == plain(sa=None) == plain(W=None) == plain(sw=None) == plain(out=None) == plain(kind=4) == plain(kind=-1) == 1
     assert plain(K=0) == plain(K=64) == plain(K=192, lda=256, ldw=256) == plain(K=131072, lda=131072, ldw=131072) == plain(K=256) == 2
     assert plain(lda=136) == plain(ldw=136) == plain(lda=1 << 22) == plain(ldw=1 << 22) == plain(M=-1) == plain(N=-1) == 2
-    assert plain(ldc=4) == plain(ldc=12) == plain(N=5, kind=1, ldc=6) == plain(A=264) == plain(W=264) == plain(out=264) == plain(work=264, n=1 << 20) == 2
+    assert plain(ldc=4) == plain(ldc=12) == plain(N=5, kind=1, ldc=6) == plain(A=264) == plain(W=264) == plain(out=264) == plain(work=264, n=1 << 20) == plain(sa=258) == plain(sw=258) == plain(M=1 << 30, N=1 << 30, ldc=1 << 30) == 2
     assert plain(M=0) == plain(N=0) == pair(M=0) == tr(M=0) == 0
     assert pair(up=None) == pair(us=None) == 1 and pair(up=264) == pair(ld=112) == pair(ldc=12) == pair(ldc=0) == 2
-    assert tr(col=None) == 1 and tr(ldo=0) == tr(ldo=12) == tr(out=264) == 2
+    assert tr(col=None) == 1 and tr(ldo=0) == tr(ldo=12) == tr(out=264) == tr(col=258) == 2
     for sizes in ((0, 8, 128), (4, 0, 128), (4, 8, 100), (4, 8, 131072), (1 << 30, 1 << 30, 128)):
         assert Q.dit_op_gemm_i8_tile(*sizes, 0, 0, None) == -1 and Q.dit_op_gemm_i8_work_bytes(*sizes, 0) == 0
     # four by thirty-two tiles of 128x128 in two shares of 64 KB each, with as much scratch; without, no shares
