@@ -499,9 +499,9 @@ def test_chain_on_a_stream_and_in_a_graph(torch, Q, M):
     m.run(Q)
     torch.cuda.synchronize()
     want = m.x.clone()
+    m.x.zero_()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    m.x.zero_()
     with torch.cuda.stream(side):
         m.run(Q, side.cuda_stream)
     side.synchronize()
