@@ -171,6 +171,8 @@ __device__ __forceinline__ void tile_coords(const P& p, int t, int& tm, int& tn)
 // K) are one stream, so the next tile's first slabs arrive under the epilogue.
 // Operands are swapped (W in the place of the MFMA's rows, its rows in the order {0-3, 8-11, ...}, {4-7, ...}), which gives a lane
 // 8 neighbouring columns of one row; tiles of transposed results keep the first order with the rows of A permuted.
+//   Bound: the matrix cores at the clock that the board's power leaves them.  8192^3 380 us, 2.89 POP/s, matrix cores busy in 87 % of the
+// cycles at 1.44 GHz; 8000 x 12288 x 4096 304 us as bf16, 336 as fp32.  (128x128 tiles: what a CU pulls, 32 KB in 0.36 to 0.48 us.)
 template <int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
   Problem& P = *(Problem*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -704,6 +706,10 @@ __global__ __launch_bounds__(256) void reduce_i8_kernel(const GemmI8 P) {
 // A workgroup owns 16 NT columns (of a pair: 8 NT of each product) and 16 MT rows.  Its waves take every WV-th slab of
 // 128 codes, so that together they read runs of WV * 128 bytes of every weight row, each exactly once.  Every wave has an LDS
 // ring of its own, D slabs deep, and waits for nobody: no barrier until the waves' sums meet in LDS.  One launch, no scratch.
+//   Bound: what a CU pulls through its L1, (MT + NT) 2 KB a slab at 85 GB/s, and HBM for the fewest rows.  1 x 12288 x 4096 9.4 us (5.3 TB/s of
+// weights in the memory-side cache; 11.7 from HBM), 32 x 12288 x 4096 10.2 (13.0), 32 x 4096 x 10240 9.8 (14), 128 x 4096 x 4096 7.6.
+//   Through LDS because a load then covers 8 rows x 128 bytes; straight into fragment order, 16 rows x 64 bytes, its addresses cost
+// four times as much (32 x 4096 x 10240 15.8 us; the weights alone straight, with twice of them in flight, 10.7).
 // Waves of a workgroup: as many slabs in flight as LDS holds (up to 8 for each wave); eight waves have 256 registers each, four have 512.
 constexpr int stream_waves(int mt, int nt) {
   const int slab = (mt + nt) * 2048, regs = mt * nt * 4 + (mt + nt) * 10 + 24;

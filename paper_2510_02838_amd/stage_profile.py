@@ -28,7 +28,7 @@ each for the stages before and after it:
     python -m paper_2510_02838_amd.stage_profile decode [--decoder ae_kl] [--res 128,256,512,1024] [--max-batch 8]
     python -m paper_2510_02838_amd.stage_profile decode --decoder vae3d [--res 256x384,512x768] [--frames 1,5,13]
           (the causal video decoder, one video per call: latency against the number of latent frames)
-    python -m paper_2510_02838_amd.stage_profile pipeline [--workload sd3|flux] [--res 512,1024] [--steps 28] [--overlap N]
+    python -m paper_2510_02838_amd.stage_profile pipeline [--workload sd3|flux] [--res 512,1024] [--steps 28] [--overlap N] [--int8]
     python -m paper_2510_02838_amd.stage_profile pipeline --workload wan --res 81x512x768 --steps 2   (video: causal video decoder)
 
   pipeline  one request through all three stages on this GPU, the output of each feeding the next
@@ -173,22 +173,24 @@ def run_grid(args):
         print(f"| {spec} | {row['tokens']} | {t:.5f} | {1.0 / t:.2f} | {ws / 2**30:.3f} | {wbytes / 2**30:.2f} |", file=sys.stderr)
 
 
-def run_encode(args):
-    import torch
-    import synth
-    from . import encoder as X
-    arch = synth.ENCODERS[args.encoder]
-    lens_list = [int(v) for v in args.lens.split(",")]
-    batches = [b for b in (1, 2, 4, 8, 16, 32, 64, 128) if b <= args.max_batch]
-    if args.int8:
-        from . import int8
-        m = int8.EncoderI8(arch)
-    else:
-        m = X.Encoder(arch)
-    m.ensure_workspace([max(lens_list)] * max(batches))
+def _encoder(args, arch, lens, **kw):
+    """An encoder with seeded weights and a workspace for `lens`; with --int8 its products run on 8-bit codes."""
+    from . import encoder, int8
+    m = (int8.EncoderI8 if args.int8 else encoder.Encoder)(arch, **kw)
+    m.ensure_workspace(lens)
     m.init_weights(1, 0.02)
     if args.int8:
         m.quantize()
+    return m
+
+
+def run_encode(args):
+    import torch
+    import synth
+    arch = synth.ENCODERS[args.encoder]
+    lens_list = [int(v) for v in args.lens.split(",")]
+    batches = [b for b in (1, 2, 4, 8, 16, 32, 64, 128) if b <= args.max_batch]
+    m = _encoder(args, arch, [max(lens_list)] * max(batches))
     wbytes = m.code_bytes() if args.int8 else m.weight_bytes()
     floor_ms = wbytes / 8e12 * 1e3
     rows = []
@@ -377,7 +379,7 @@ def run_decode(args):
 def run_pipeline(args):
     import torch
     import synth
-    from . import encoder as XE, decoder as XD
+    from . import decoder as XD
     st = Stage(args.workload, args.steps)
     arch = st.arch
     video = arch["family"] == "W"            # video latents [C][F][h][w] go to the causal video decoder
@@ -388,10 +390,8 @@ def run_pipeline(args):
     specs = args.res.split(",")
     reqs = [[_latent_dims(st.cfg, r) + (st.n_cond,)] for r in specs]
     st.prepare(reqs)
-    enc = XE.Encoder(enc_arch)
     lens = [st.n_cond]
-    enc.ensure_workspace(lens)
-    enc.init_weights(1, 0.02)
+    enc = _encoder(args, enc_arch, lens)
     dec = XD.Decoder(dec_arch)
     big = max(reqs, key=lambda r: dec.workspace_bytes(r[0][1], r[0][2], r[0][0]))[0]
     if min(dec.workspace_bytes(r[0][1], r[0][2], r[0][0]) for r in reqs) == 0:
@@ -455,7 +455,7 @@ def _overlap(args, spec, rq):
     """N requests of one shape: the three stages on three streams against one stream."""
     import torch
     import synth
-    from . import encoder as XE, decoder as XD
+    from . import decoder as XD
     N = args.overlap
     enc_arch, dec_arch = synth.ENCODERS["t5_xxl"], synth.DECODERS["ae_kl"]
     _, h, w, n_cond = rq[0]
@@ -466,8 +466,7 @@ def _overlap(args, spec, rq):
         st = Stage(args.workload, args.steps, stream=sd.cuda_stream)
         st.prepare([rq])
         arch = st.arch
-        enc = XE.Encoder(enc_arch, stream=se.cuda_stream)
-        enc.ensure_workspace([n_cond]); enc.init_weights(1, 0.02)
+        enc = _encoder(args, enc_arch, [n_cond], stream=se.cuda_stream)
         dec = XD.Decoder(dec_arch, stream=sc.cuda_stream)
         dec.ensure_workspace(h, w); dec.init_weights(1, 0.02)
         f = dec.up_factor()
@@ -528,7 +527,7 @@ def main():
     ap.add_argument("--frames", default="1,5,13", help="decode with a video decoder: latent frames per video")
     ap.add_argument("--encoder", default="t5_xxl", choices=["t5_xxl", "t5_tiny"])
     ap.add_argument("--lens", default="32,128,500")
-    ap.add_argument("--int8", action="store_true", help="encode: the products on 8-bit integers")
+    ap.add_argument("--int8", action="store_true", help="encode, pipeline: the encoder's products on 8-bit integers")
     ap.add_argument("--workload", default="sd3", choices=["sd3", "flux", "wan", "tiny"])
     ap.add_argument("--res", default=None)
     ap.add_argument("--steps", type=int, default=None, help="denoising steps per timed sample")
