@@ -939,16 +939,24 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
 // 7.6, 128x128 14; 200 rows, N = 12288 128x128 20, stream 23; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
 // 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Two shares of K: 500 rows, N = 4096,
 // K = 10240 30.7, unsplit 36, stream 34; 248 rows, N = 6176, K = 9600 27 % less than anything unsplit.
-struct Choice { int variant, splits; };
-Choice choose(int M, int N, int K, bool pair, size_t scratch) {
+//   Columns that fill whole rounds of 256 8-wave tiles go ahead of the rest, which then takes the tile that suits it, where that saves 5 %:
+// 528 tiles are two rounds and 16 tiles more.  2744 x 12288 x 4096 138 -> 125 us, a gated pair of 1000 x 10240 x 4096 92 -> 79; without the
+// 5 % 2200 x 4096 x 10240 89 -> 94.
+struct Choice { int variant, splits; float us; };
+struct Plan { Choice main, rest; int first; };      // first: columns of the main launch where the rest has one of its own, else 0
+
+struct Tile { int bm, bn; float one, all, on, fixed; };            // a slab of the only tile, of 256 tiles, of round after round
+constexpr Tile TILES[] = {{128, 128, 0.305f, 0.458f, 0.477f, 3.3f}, {128, 256, 0.43f, 0.70f, 0.75f, 5.7f},
+                          {256, 128, 0.43f, 0.70f, 0.75f, 5.7f}, {256, 256, 0.70f, 1.19f, 1.29f, 9.6f}};
+
+// cols: columns of the product, of a pair those of both
+Choice choose(int M, long long cols, int K, bool pair, size_t scratch) {
   const int nk = K / 128;
-  const long long cols = pair ? 2LL * N : N;
-  const float least = 0.4f + ((float)M * K + (float)cols * K + 2.f * M * N) / 4.8e6f;
-  Choice best = {0, 1};
-  float best_us = 0.f;
+  const float least = 0.4f + ((float)M * K + (float)cols * K + (pair ? 1.f : 2.f) * M * cols) / 4.8e6f;
+  Choice best = {0, 1, 0.f};
   auto offer = [&](int variant, int splits, float us) {
     if (us < least) us = least + us * 1e-3f;
-    if (!best.variant || us < best_us) { best = Choice{variant, splits}; best_us = us; }
+    if (!best.variant || us < best.us) best = Choice{variant, splits, us};
   };
   // (most rows first: at the same estimate two row tiles of one workgroup read a weight once, two workgroups twice; cold weights,
   // 32 rows, N = 4096, K = 10240: 13.7 us with 32 x 16 tiles, 14.7 with 16 x 32)
@@ -959,11 +967,8 @@ Choice choose(int M, int N, int K, bool pair, size_t scratch) {
       if (wgs > (1 << 22)) continue;                                                        // (512 threads each: a launch has less than 2^32)
       offer(100 * mt + nt, 1, 0.6f + (float)rounds * (nk * (0.0141f * (mt + nt) + 0.005f * mt * nt) + (rounds > 1 ? 1.95f : 2.9f) + 0.054f * mt * nt));
     }
-  struct Tile { int bm, bn; float one, all, on, fixed; };          // a slab of the only tile, of 256 tiles, of round after round
-  static constexpr Tile tiles[] = {{128, 128, 0.305f, 0.458f, 0.477f, 3.3f}, {128, 256, 0.43f, 0.70f, 0.75f, 5.7f},
-                                   {256, 128, 0.43f, 0.70f, 0.75f, 5.7f}, {256, 256, 0.70f, 1.19f, 1.29f, 9.6f}};
   auto slab = [](const Tile& t, long long n) { return t.one + (t.all - t.one) * (float)n / 256.f; };
-  for (const Tile& t : tiles) {
+  for (const Tile& t : TILES) {
     const long long n = (M + t.bm - 1LL) / t.bm * ((cols + t.bn - 1) / t.bn), full = n > 256 ? n / 256 : 0, rest = n - full * 256;
     offer(t.bm * 1000 + t.bn, 1, 2.6f + (float)full * (nk * t.on + t.fixed) + (rest ? nk * slab(t, rest) + t.fixed : 0.f));
   }
@@ -971,8 +976,24 @@ Choice choose(int M, int N, int K, bool pair, size_t scratch) {
   const long long n = (M + 127LL) / 128 * ((cols + 127) / 128);
   for (int s = 2; s <= 4 && n * s <= 256 && nk >= 8 * s; ++s)
     if ((size_t)n * s * (128 * 128 * 4) <= scratch)
-      offer(128128, s, 5.3f + (float)((nk + s - 1) / s) * slab(tiles[0], n * s) + 2.3f + (float)n * s * 0.018f);
+      offer(128128, s, 5.3f + (float)((nk + s - 1) / s) * slab(TILES[0], n * s) + 2.3f + (float)n * s * 0.018f);
   return best;
+}
+
+Plan make_plan(int M, int N, int K, bool pair, size_t scratch) {
+  const long long cols = pair ? 2LL * N : N;
+  Plan p = {choose(M, cols, K, pair, scratch), {0, 1, 0.f}, 0};
+  float best = p.main.us * 0.95f;
+  for (const Tile& t : TILES) {
+    const long long tm = (M + t.bm - 1LL) / t.bm, n = tm * ((cols + t.bn - 1) / t.bn), full = n / 256;
+    if (full < 1 || n % 256 == 0) continue;
+    const long long first = full * 256 / tm * t.bn / 256 * 256;      // (256: transposed columns of the rest start at one of its tiles)
+    if (first <= 0 || first >= cols) continue;
+    const Choice rest = choose(M, cols - first, K, pair, scratch);
+    const float us = 2.6f + (float)full * (K / 128 * (full > 1 ? t.on : t.all) + t.fixed) + rest.us;
+    if (us < best) { best = us; p.main = Choice{t.bm * 1000 + t.bn, 1, us}; p.rest = rest; p.first = (int)(pair ? first / 2 : first); }
+  }
+  return p;
 }
 
 }  // namespace
@@ -997,20 +1018,39 @@ bool launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant) {
   return false;
 }
 
-int gemm_i8_variant(int M, int N, int K, bool pair, size_t scratch, int* splits) {
-  const Choice c = choose(M, N, K, pair, scratch);
-  *splits = c.splits;
-  return c.variant;
+int gemm_i8_plan(int M, int N, int K, bool pair, size_t scratch, int (&out)[3]) {
+  const Plan p = make_plan(M, N, K, pair, scratch);
+  out[0] = p.main.splits; out[1] = p.first; out[2] = p.rest.variant;
+  return p.main.variant;
 }
 size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {
-  const Choice c = choose(M, N, K, pair, ~(size_t)0);
-  return c.splits == 1 ? 0 : (size_t)((M + 127) / 128) * (((pair ? 2LL * N : N) + 127) / 128) * c.splits * (128 * 128 * 4);
+  const Plan p = make_plan(M, N, K, pair, ~(size_t)0);
+  const Choice& c = p.first ? p.rest : p.main;
+  const long long n = N - p.first;
+  return c.splits == 1 ? 0 : (size_t)((M + 127) / 128) * (((pair ? 2 * n : n) + 127) / 128) * c.splits * (128 * 128 * 4);
 }
 
 void launch_gemm_i8(hipStream_t s, GemmI8& p) {
-  const Choice c = choose(p.M, p.N, p.K, p.W2 != nullptr, p.partial ? p.partial_bytes : 0);
-  p.splits = c.splits;
-  launch_gemm_i8_variant(s, p, c.variant);
+  const Plan plan = make_plan(p.M, p.N, p.K, p.W2 != nullptr, p.partial ? p.partial_bytes : 0);
+  const int n1 = plan.first;
+  if (!n1) {
+    p.splits = plan.main.splits;
+    launch_gemm_i8_variant(s, p, plan.main.variant);
+    return;
+  }
+  GemmI8 a = p, b = p;                                   // columns 0 .. n1 - 1, and the rest
+  a.N = n1; a.splits = 1;
+  if (a.vt_from > n1) a.vt_from = n1;
+  b.N = p.N - n1; b.splits = plan.rest.splits;
+  b.W += (size_t)n1 * p.ldw; b.sw += n1;
+  if (b.W2) { b.W2 += (size_t)n1 * p.ldw; b.sw2 += n1; }
+  if (b.bias) b.bias += n1;
+  if (b.gate) b.gate += n1;
+  if (b.out) b.out = (char*)b.out + (size_t)n1 * (p.kind == OUT_F32 || p.kind == OUT_RESID_F32 ? 4 : 2);
+  if (p.vt_from < n1) { b.vt += (size_t)(n1 - p.vt_from) * p.ldvt; b.vt_from = 0; }
+  else b.vt_from = p.vt_from - n1;
+  launch_gemm_i8_variant(s, a, plan.main.variant);
+  launch_gemm_i8_variant(s, b, plan.rest.variant);
 }
 
 }  // namespace dit

@@ -107,11 +107,11 @@ static bool sizes_ok(int M, int N, int K) { return M > 0 && N > 0 && K > 0 && K 
 
 size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair) { return sizes_ok(M, N, K) ? gemm_i8_work_bytes(M, N, K, pair != 0) : 0; }
 
-int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* splits) {
+int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* plan) {
   if (!sizes_ok(M, N, K)) return -1;
-  int s = 1;
-  const int tile = gemm_i8_variant(M, N, K, pair != 0, work_bytes, &s);
-  if (splits) *splits = s;
+  int p[3];
+  const int tile = gemm_i8_plan(M, N, K, pair != 0, work_bytes, p);
+  for (int i = 0; plan && i < 3; ++i) plan[i] = p[i];
   return tile;
 }
 

@@ -71,11 +71,11 @@ def test_products_check_their_arguments(Q):
     for sizes in ((0, 8, 128), (4, 0, 128), (4, 8, 100), (4, 8, 131072), (1 << 30, 1 << 30, 128)):
         assert Q.dit_op_gemm_i8_tile(*sizes, 0, 0, None) == -1 and Q.dit_op_gemm_i8_work_bytes(*sizes, 0) == 0
     # four by thirty-two tiles of 128x128 in two shares of 64 KB each, with as much scratch; without, no shares
-    n, s = Q.C.c_int(), 4 * 32 * 2 * 65536
+    n, s = (Q.C.c_int * 3)(), 4 * 32 * 2 * 65536
     assert Q.dit_op_gemm_i8_work_bytes(500, 4096, 10240, 0) == s
-    assert Q.dit_op_gemm_i8_tile(500, 4096, 10240, 0, s, n) == 128128 and n.value == 2
+    assert Q.dit_op_gemm_i8_tile(500, 4096, 10240, 0, s, n) == 128128 and list(n) == [2, 0, 0]
     Q.dit_op_gemm_i8_tile(500, 4096, 10240, 0, s - 1, n)
-    assert n.value == 1
+    assert n[0] == 1
     with pytest.raises(Exception, match="DIT_ESHAPE"):
         Q.check(2)
 
@@ -295,18 +295,26 @@ PAIRS = {102: (3, 5, 128), 104: (1, 4128, 128), 106: (1, 8203, 128), 202: (4101,
          (16480, 1, 128), 504: (19688, 17, 128), 506: (67, 8335, 128), 602: (3374, 97, 128), 604: (10372, 50, 128), 128128: (1, 10609,
          4352), 128256: (38, 26248, 128), 256128: (162, 9909, 128), 256256: (137, 18938, 128)}
 
+# two launches: whole rounds of 8-wave tiles, and the columns behind them
+TWO = [(392, 16523, 256), (921, 16563, 128), (1031, 15287, 128)]
+TWO_PAIRS = [(262, 11076, 256), (386, 16961, 128), (518, 13676, 128)]
+
 
 def test_every_tile_is_tested(Q):
     """The lists above reach what they say, and no drawn shape takes a tile that they leave out."""
     for pair, table in ((0, TILES), (1, PAIRS)):
         assert {t: Q.dit_op_gemm_i8_tile(*s, pair, 0, None) for t, s in table.items()} == {t: t for t in table}
         rng = np.random.RandomState(pair)
+        plan = (Q.C.c_int * 3)()
+        for s in TWO_PAIRS if pair else TWO:
+            assert Q.dit_op_gemm_i8_tile(*s, pair, 0, plan) > 1000 and 0 < plan[1] < s[1] and plan[2] in table
         for M, N, K in zip(*(np.exp(rng.uniform(0, math.log(m), 3000)).astype(int) for m in (20000, 40000, 160))):
-            assert Q.dit_op_gemm_i8_tile(int(M), int(N), 128 * int(K), pair, 0, None) in table
+            assert Q.dit_op_gemm_i8_tile(int(M), int(N), 128 * int(K), pair, 0, plan) in table
+            assert plan[0] == 1 and 0 <= plan[1] < N and (plan[2] in table if plan[1] else plan[2] == 0)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", SHAPES + list(TILES.values()))
+@pytest.mark.parametrize("M,N,K", SHAPES + list(TILES.values()) + TWO)
 def test_product_of_codes_in_every_form(torch, Q, M, N, K):
     P = Product(torch, M, N, K, seed=M + N + K, pad_a=48, pad_w=16)
     p, b = P.exact(), P.bias.double()
@@ -337,7 +345,7 @@ def test_product_of_codes_in_every_form(torch, Q, M, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", SHAPES + list(PAIRS.values()))
+@pytest.mark.parametrize("M,N,K", SHAPES + list(PAIRS.values()) + TWO_PAIRS)
 def test_gated_pair_of_codes(torch, Q, M, N, K):
     P = Product(torch, M, N, K, seed=M + N + K, pad_a=16, pad_w=32, pair=True)
     g, u = P.exact(), P.exact(P.W2, P.sw2)
@@ -373,7 +381,7 @@ def columns(M, kind):
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["ragged", "packed", "odd", "sparse"])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 128), (1, 300, 256), (17, 520, 2048), (32, 4096, 512), (64, 256, 4096), (77, 1030, 512), (130, 512, 640), (300, 768, 1280), (511, 4096, 256),
-                                   (1137, 2048, 256), (2049, 1100, 128)])
+                                   (1137, 2048, 256), (2049, 1100, 128), (392, 16523, 256)])
 def test_product_of_codes_transposed(torch, Q, kind, M, N, K):
     P = Product(torch, M, N, K, seed=M + N + K, pad_a=16)
     c = columns(M, kind)
