@@ -89,11 +89,12 @@ def codes_of(y):
 
 def run_quantize(torch, Q, x, d, ldq=None, stream=None):
     M, ldq = x.shape[0], ldq or up(d, 128)
-    codes = torch.full((M, ldq), 77, dtype=torch.int8, device="cuda")
-    scale = torch.full((M,), -1.0, device="cuda")
+    codes = torch.full((M + 3, ldq), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((M + 3,), -1.0, device="cuda")
     Q.check(Q.dit_op_quantize_i8(stream, x.data_ptr(), int(x.dtype == torch.float32), x.stride(0), M, d, codes.data_ptr(), ldq, scale.data_ptr()))
     torch.cuda.synchronize()
-    return codes.cpu().numpy(), scale.cpu().numpy()
+    assert bool((codes[M:] == 77).all()) and bool((scale[M:] == -1.0).all())             # (rows behind the last)
+    return codes[:M].cpu().numpy(), scale[:M].cpu().numpy()
 
 
 @pytest.mark.gpu
@@ -135,14 +136,15 @@ def test_quantize_of_extreme_rows(torch, Q):
 
 def run_norm(torch, Q, x, delta, gain, d, eps=1e-6, x_out=None, ldq=None, stream=None):
     M, ldq = x.shape[0], ldq or up(d, 128)
-    codes = torch.full((M, ldq), 77, dtype=torch.int8, device="cuda")
-    scale = torch.full((M,), -1.0, device="cuda")
+    codes = torch.full((M + 3, ldq), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((M + 3,), -1.0, device="cuda")
     Q.check(Q.dit_op_rmsnorm_i8(stream, x.data_ptr(), x.stride(0), None if delta is None else delta.data_ptr(),
                                 int(delta is not None and delta.dtype == torch.float32), 0 if delta is None else delta.stride(0), gain.data_ptr(), eps,
                                 M, d, None if x_out is None else x_out.data_ptr(), 0 if x_out is None else x_out.stride(0), codes.data_ptr(), ldq,
                                 scale.data_ptr()))
     torch.cuda.synchronize()
-    return codes.cpu().numpy(), scale.cpu().numpy()
+    assert bool((codes[M:] == 77).all()) and bool((scale[M:] == -1.0).all())
+    return codes[:M].cpu().numpy(), scale[:M].cpu().numpy()
 
 
 def check_norm(codes, scale, xs, gain, d, eps=1e-6):
@@ -233,32 +235,35 @@ class Product:
         f32 = kind in (1, 3)
         ldc = up(self.N, 8) + 8
         if out is None:
-            out = torch.full((A.shape[0], ldc), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+            out = torch.full((A.shape[0] + 3, ldc), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
         Q.check(Q.dit_op_gemm_i8(stream, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.W.stride(0), self.sw.data_ptr(),
                                  self.bias.data_ptr() if bias else None, A.shape[0], self.N, self.K, kind, out.data_ptr(), ldc,
                                  None if gate is None else gate.data_ptr(), 0 if gate is None else gate.stride(0),
                                  None if row_req is None else row_req.data_ptr(), self.work.data_ptr() if work else None,
                                  self.work.numel() * 4 if work else 0))
-        return out
+        assert out.shape[0] == A.shape[0] or bool((out[A.shape[0]:] == 9.0).all())         # (rows behind the last)
+        return out[:A.shape[0]]
 
     def pair(self, Q, rows=slice(None), work=True):
         torch = self.torch
         A, sa = self.A[rows], self.sa[rows]
         ldc = up(self.N, 8) + 8
-        out = torch.full((A.shape[0], ldc), 9.0, dtype=torch.bfloat16, device="cuda")
+        out = torch.full((A.shape[0] + 3, ldc), 9.0, dtype=torch.bfloat16, device="cuda")
         Q.check(Q.dit_op_gemm_i8_geglu(None, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.sw.data_ptr(), self.W2.data_ptr(),
                                        self.sw2.data_ptr(), self.W.stride(0), A.shape[0], self.N, self.K, out.data_ptr(), ldc,
                                        self.work.data_ptr() if work else None, self.work.numel() * 4 if work else 0))
-        return out
+        assert bool((out[A.shape[0]:] == 9.0).all())
+        return out[:A.shape[0]]
 
     def transposed(self, Q, col, ldo, bias=True, rows=slice(None), work=True):
         torch = self.torch
         A, sa = self.A[rows], self.sa[rows]
-        out = torch.full((self.N, ldo), 9.0, dtype=torch.bfloat16, device="cuda")
+        out = torch.full((self.N + 3, ldo), 9.0, dtype=torch.bfloat16, device="cuda")
         Q.check(Q.dit_op_gemm_i8_transposed(None, A.data_ptr(), self.A.stride(0), sa.data_ptr(), self.W.data_ptr(), self.W.stride(0), self.sw.data_ptr(),
                                             self.bias.data_ptr() if bias else None, A.shape[0], self.N, self.K, out.data_ptr(), ldo, col.data_ptr(),
                                             self.work.data_ptr() if work else None, self.work.numel() * 4 if work else 0))
-        return out
+        assert bool((out[self.N:] == 9.0).all())
+        return out[:self.N]
 
 
 def gelu64(v):
