@@ -935,10 +935,11 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
 // its products; a slab of an 8-wave tile takes longer the more CUs run one (the clock falls with the matrix load: 256x256 0.7 us for
 // one, 1.2 with all of them busy, 1.3 round after round).  Nothing is faster than its bytes at 4.8 TB/s.
 // The constants were fitted to 312 products of 1 to 8000 rows, 300 to 12288 columns and K from 512 to 10240 with every variant timed: the
-// one chosen took 1.005 times the best one's time in the mean, 1.07 at most.  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
+// one chosen took 1.005 times the best one's time in the mean, 1.09 at most; over 140 other shapes 1.013 and 1.13 (the most where a last
+// round of few tiles has a launch of its own).  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
 // 7.6, 128x128 14; 200 rows, N = 12288 128x128 20, stream 23; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
 // 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Two shares of K: 500 rows, N = 4096,
-// K = 10240 30.7, unsplit 36, stream 34; 248 rows, N = 6176, K = 9600 27 % less than anything unsplit.
+// K = 10240 31.9, unsplit 36.6, stream 39.8; 248 rows, N = 6176, K = 9600 anything unsplit takes 27 % longer.
 //   Columns that fill whole rounds of 256 8-wave tiles go ahead of the rest, which then takes the tile that suits it, where that saves 5 %:
 // 528 tiles are two rounds and 16 tiles more.  2744 x 12288 x 4096 138 -> 125 us, a gated pair of 1000 x 10240 x 4096 92 -> 79; without the
 // 5 % 2200 x 4096 x 10240 89 -> 94.
