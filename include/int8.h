@@ -42,7 +42,7 @@ dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* 
 
 /* C[m][n] = a_scale[m] * w_scale[n] * sum_k A[m][k] W[n][k] (+ bias[n]) on the 8-bit matrix cores; the sum is exact.
  * A: codes [M][lda]; W: codes [N][ldw] (no padding rows needed); a_scale: dev float32 [M]; w_scale: dev float32 [N]; bias: dev float32
- * [N] or NULL; K a multiple of 128, at most DIT_I8_MAX_K; lda, ldw multiples of 16 below 2^22.  out_kind, out, ldc, gate, gate_stride and row_req
+ * [N] or NULL; K a multiple of 128, at most DIT_I8_MAX_K; lda, ldw multiples of 16 below 2^22; ldc below 2^26.  out_kind, out, ldc, gate, gate_stride and row_req
  * as for dit_op_gemm (0 bf16, 1 float32, 2 bf16 of tanh-GELU, 3 float32 out += gate * C); any code -128..127 is
  * taken.  The result does not depend on how the product is cut up: it is the same, bit for bit, alone or among other rows.
  * work: dev scratch for the shares of a product that is split along K between workgroups (dit_op_gemm_i8_work_bytes says how much the
@@ -52,7 +52,7 @@ dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_s
                           const float* bias, int M, int N, int K, int out_kind, void* out, int ldc, const float* gate,
                           int gate_stride, const int* row_req, void* work, size_t work_bytes);
 
-/* bf16 of tanh-GELU(product with W_gate) * (product with W_up), both [N][ldw]. */
+/* bf16 of tanh-GELU(product with W_gate) * (product with W_up), both [N][ldw]; ldc below 2^26. */
 dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const float* a_scale, const void* W_gate, const float* gate_scale,
                                 const void* W_up, const float* up_scale, int ldw, int M, int N, int K, void* out, int ldc,
                                 void* work, size_t work_bytes);

@@ -13,6 +13,9 @@ inline dit_status launched() { return hipGetLastError() == hipSuccess ? DIT_OK :
 // (tiles and shares are counted in 32 bits)
 inline bool countable(int M, int N) { return M <= (1 << 30) && N <= (1 << 30) && (M + 127LL) / 128 * ((N + 15LL) / 16) < (1LL << 26); }
 
+// (a tile's results are stored at 32-bit byte offsets from its first row: up to 15 rows of bf16 or 7 of float32)
+constexpr int MAX_LDC = 1 << 26;
+
 // what the three forms of the product have in common
 dit_status check_product(const void* A, int lda, const float* a_scale, const void* W, int ldw, const float* w_scale, int M, int N, int K,
                          const void* out, const void* work) {
@@ -66,7 +69,7 @@ dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_s
   const dit_status st = check_product(A, lda, a_scale, W, ldw, w_scale, M, N, K, out, work);
   if (st != DIT_OK) return st;
   if (out_kind < OUT_BF16 || out_kind > OUT_RESID_F32) return DIT_EINVAL;
-  if (ldc < N || ldc % (out_kind == OUT_F32 || out_kind == OUT_RESID_F32 ? 4 : 8) || off4(bias)) return DIT_ESHAPE;
+  if (ldc < N || ldc >= MAX_LDC || ldc % (out_kind == OUT_F32 || out_kind == OUT_RESID_F32 ? 4 : 8) || off4(bias)) return DIT_ESHAPE;
   if (out_kind == OUT_RESID_F32 && (off4(gate) || off4(row_req))) return DIT_ESHAPE;
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W, ldw, w_scale, bias, M, N, K, out_kind, out, ldc, work, work_bytes);
@@ -81,7 +84,7 @@ dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const floa
   const dit_status st = check_product(A, lda, a_scale, W_gate, ldw, gate_scale, M, N, K, out, work);
   if (st != DIT_OK) return st;
   if (!W_up || !up_scale) return DIT_EINVAL;
-  if (ldc < N || ldc % 8 || off16(W_up) || off4(up_scale)) return DIT_ESHAPE;
+  if (ldc < N || ldc >= MAX_LDC || ldc % 8 || off16(W_up) || off4(up_scale)) return DIT_ESHAPE;
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W_gate, ldw, gate_scale, nullptr, M, N, K, OUT_BF16, out, ldc, work, work_bytes);
   p.W2 = (const int8_t*)W_up; p.sw2 = up_scale;

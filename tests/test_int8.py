@@ -81,6 +81,17 @@ def test_products_check_their_arguments(Q):
 
 
 # ------------------------------------------------------------------------------------------------ rows to codes
+def test_rows_of_results_past_32_bit_offsets_are_refused(Q):
+    """A tile's results are addressed by 32-bit byte offsets from its first row: at most 15 ldc bf16 or 7 ldc float32 elements, which
+    2^32 bytes hold below ldc = 2^26 and no longer hold at 2^28.  (M = 0: the arguments are checked and nothing is launched.)"""
+    p = 1 << 20
+    for ldc, ok in (((1 << 26) - 8, True), (1 << 26, False), (1 << 28, False), ((1 << 31) - 8, False)):
+        want = Q.DIT_OK if ok else next(k for k, v in Q.STATUS_NAMES.items() if v == "DIT_ESHAPE")
+        for kind in range(4):
+            assert Q.dit_op_gemm_i8(None, p, 128, p, p, 128, p, None, 0, 8, 128, kind, p, ldc, None, 0, None, None, 0) == want
+        assert Q.dit_op_gemm_i8_geglu(None, p, 128, p, p, p, p, p, 128, 0, 8, 128, p, ldc, None, 0) == want
+
+
 def codes_of(y):
     """Scales and exact quotients of float64 rows."""
     s = np.maximum((np.abs(y).max(axis=1) / 127.0).astype(np.float32), np.float32(TINY))
