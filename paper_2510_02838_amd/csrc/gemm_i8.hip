@@ -942,7 +942,8 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
 // K = 10240 31.9, unsplit 36.6, stream 39.8; 248 rows, N = 6176, K = 9600 anything unsplit takes 27 % longer.
 //   Columns that fill whole rounds of 256 8-wave tiles go ahead of the rest, which then takes the tile that suits it, where that saves 5 %:
 // 528 tiles are two rounds and 16 tiles more.  2744 x 12288 x 4096 138 -> 125 us, a gated pair of 1000 x 10240 x 4096 92 -> 79; without the
-// 5 % 2200 x 4096 x 10240 89 -> 94.
+// 5 % 2200 x 4096 x 10240 89 -> 94.  160 drawn shapes where it is chosen: 0.76 to 1.10 of the best 8-wave tile in one launch, 0.944 in the
+// mean; 1 us for the second launch in the estimate would win 0.1 %, more of it or a larger margin lose.
 struct Choice { int variant, splits; float us; };
 struct Plan { Choice main, rest; int first; };      // first: columns of the main launch where the rest has one of its own, else 0
 
