@@ -1,0 +1,184 @@
+"""Products of codes in shares of K, in two launches, and transposed on every tile: the calls that the shapes of test_int8.py do not
+reach.  Each list says what its shapes take, and a host test holds it to that."""
+import numpy as np
+import pytest
+
+import synth
+from test_int8 import (BF16, F32, TILES, TWO, Product, columns, gelu64, gelu_bound, product_bound, up,
+                       Q, torch)  # noqa: F401 (the last two are fixtures)
+
+SCRATCH = 32 << 20                        # what Product passes
+
+# shape: shares of K, columns of a first launch
+SHARED = {(500, 4096, 10240): (2, 0), (102, 9736, 9728): (3, 0), (104, 6200, 10240): (4, 0), (85, 6203, 20480): (4, 0), (339, 3099, 20480): (3, 0),
+          (700, 1537, 20480): (3, 0), (241, 3101, 10240): (4, 0)}
+SHARED_PAIRS = {(104, 6200, 5120): (2, 0), (257, 1536, 20480): (3, 0), (104, 3080, 10240): (4, 0), (225, 1030, 20480): (4, 0), (397, 1023, 20480): (4, 0),
+                (1473, 521, 10240): (2, 0)}
+# ... of the second of two launches
+SHARED_REST = {(2562, 6654, 5376): (2, 5888), (1130, 8282, 10880): (3, 7168), (1638, 5351, 11904): (4, 4864)}
+SHARED_REST_PAIRS = {(3368, 2559, 4992): (2, 2304), (869, 5362, 9856): (3, 4608), (1226, 3516, 10880): (4, 3200)}
+# many rows to transpose: tiles of 256 rows with ragged last ones
+TALL = {(1928, 2600, 8064): 256128, (3955, 3186, 1536): 256256}
+
+
+def shares(Q, M, N, K, pair, scratch=SCRATCH):
+    """(shares of K of the launch that is split, columns of a first launch): the scratch says how many, 64 KB for each tile and share."""
+    plan = (Q.C.c_int * 3)()
+    assert Q.dit_op_gemm_i8_tile(M, N, K, pair, scratch, plan) > 0
+    need = Q.dit_op_gemm_i8_work_bytes(M, N, K, pair)
+    assert need <= SCRATCH
+    cols = (2 if pair else 1) * (N - plan[1])
+    return (need // (-(-M // 128) * -(-cols // 128) * 65536) if need else 1), plan[1]
+
+
+def test_the_shapes_take_what_their_lists_say(Q):
+    for pair, tables in ((0, (SHARED, SHARED_REST)), (1, (SHARED_PAIRS, SHARED_REST_PAIRS))):
+        for table in tables:
+            assert {s: shares(Q, *s, pair) for s in table} == table
+            assert {n for n, _ in table.values()} == {2, 3, 4}
+    assert {s: Q.dit_op_gemm_i8_tile(*s, 0, SCRATCH, None) for s in TALL} == TALL
+    assert shares(Q, 128, 2176, Q.MAX_K, 0) == shares(Q, 128, 1088, Q.MAX_K, 1) == (4, 0)
+    assert Q.dit_op_gemm_i8_tile(500, 4096, 15360, 0, 0, None) > 1000                                     # (8-wave tiles, unsplit)
+    assert shares(Q, 1100, 3100, 20480, 0) == (1, 0) and {shares(Q, n, 3100, 20480, 0)[0] for _, n in PARTS} == {1, 2, 3, 4}
+    assert shares(Q, 1100, 1030, 20480, 1) == (1, 0) and {shares(Q, n, 1030, 20480, 1)[0] for _, n in PARTS} == {1, 2, 3, 4}
+    # the encoder's query, key and value product at T5-XXL widths: 1793 tokens, where the first launch ends with the keys
+    assert shares(Q, 1793, 3 * 4096, 4096, 0) == (1, 2 * 4096)
+
+
+def close(got, want, tol):
+    d = (got.double() - want).abs()
+    assert bool((d <= tol).all()), float((d - tol).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", list(SHARED) + list(SHARED_REST))
+def test_products_in_shares_of_k(torch, Q, M, N, K):
+    """Every kind, with and without bias and gates, against the formula; and without scratch, unsplit, not a bit differs."""
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=48, pad_w=16)
+    p, b = P.exact(), P.bias.double()
+    for bias in (True, False):
+        v = p + b if bias else p
+        dv = product_bound(p, b if bias else 0.0 * b)
+        for kind in (0, 1, 2):
+            out = P.plain(Q, kind, bias)
+            want, tol = (gelu64(v), gelu_bound(v, dv)) if kind == 2 else (v, dv)
+            if kind != 1:
+                tol = tol + BF16 * (want.abs() + tol)
+            close(out[:, :N], want, tol)
+            assert bool((out[:, N:] == 9.0).all())
+            assert torch.equal(out, P.plain(Q, kind, bias, work=False))
+    x = torch.randn(M, up(N, 8) + 8, generator=torch.Generator().manual_seed(2)).cuda()
+    gate = torch.randn(3, N + 1, generator=torch.Generator().manual_seed(3)).cuda()
+    req = (torch.arange(M) * 3 // M).to(torch.int32).cuda()
+    for gt, rr in ((gate, req), (gate, None), (None, None)):
+        out = P.plain(Q, 3, out=x.clone(), gate=gt, row_req=rr)
+        gv = 1.0 if gt is None else gate[0, :N].double() if rr is None else gate.double()[req.long()][:, :N]
+        want = x[:, :N].double() + gv * (p + b)
+        close(out[:, :N], want, 1.01 * F32 * want.abs() + abs(gv) * product_bound(p, b))
+        assert torch.equal(out[:, N:], x[:, N:])
+        assert torch.equal(out, P.plain(Q, 3, out=x.clone(), gate=gt, row_req=rr, work=False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", list(SHARED_PAIRS) + list(SHARED_REST_PAIRS))
+def test_gated_pairs_in_shares_of_k(torch, Q, M, N, K):
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=16, pad_w=32, pair=True)
+    g, u = P.exact(), P.exact(P.W2, P.sw2)
+    zero = 0.0 * P.bias.double()
+    dg, du = gelu_bound(g, product_bound(g, zero)), product_bound(u, zero)
+    want = gelu64(g) * u
+    tol = dg * u.abs() + gelu64(g).abs() * du + dg * du
+    out = P.pair(Q)
+    close(out[:, :N], want, tol + (BF16 + F32) * (want.abs() + tol))
+    assert bool((out[:, N:] == 9.0).all())
+    assert torch.equal(out, P.pair(Q, work=False))
+
+
+def check_transposed(torch, Q, M, N, K, kind, bias):
+    P = Product(torch, M, N, K, seed=M + N + K, pad_a=16)
+    c = columns(M, kind)
+    ldo = up(int(c[-1]) + 1, 8) + 16
+    col = torch.from_numpy(c.astype(np.int32)).cuda()
+    p, b = P.exact(), P.bias.double() if bias else 0.0 * P.bias.double()
+    dv = product_bound(p, b)
+    out = P.transposed(Q, col, ldo, bias)
+    close(out[:, col.long()].t(), p + b, dv + BF16 * ((p + b).abs() + dv))
+    rest = torch.ones(ldo, dtype=torch.bool, device="cuda")
+    rest[col.long()] = False
+    assert bool((out[:, rest] == 9.0).all())
+    assert torch.equal(out, P.transposed(Q, col, ldo, bias, work=False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,bias", [("ragged", True), ("odd", False), ("sparse", True)])
+@pytest.mark.parametrize("M,N,K", list(SHARED) + list(SHARED_REST))
+def test_transposed_products_in_shares_of_k(torch, Q, M, N, K, kind, bias):
+    check_transposed(torch, Q, M, N, K, kind, bias)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,bias", [("ragged", True), ("odd", False)])
+@pytest.mark.parametrize("M,N,K", list(TILES.values()) + TWO + list(TALL))
+def test_transposed_products_on_every_tile(torch, Q, M, N, K, kind, bias):
+    check_transposed(torch, Q, M, N, K, kind, bias)
+
+
+PARTS = ((0, 1), (3, 33), (40, 100), (100, 256), (300, 350), (11, 600), (400, 700))
+
+
+@pytest.mark.gpu
+def test_a_row_is_the_same_in_any_shares_of_k(torch, Q):
+    """A product of 1100 rows, unsplit, and parts of it in other tiles and in 2, 3 and 4 shares of K: not a bit differs."""
+    P = Product(torch, 1100, 3100, 20480)
+    T = Product(torch, 1100, 1030, 20480, seed=2, pair=True)
+    col = torch.arange(1100, dtype=torch.int32, device="cuda")
+    full = {k: P.plain(Q, k) for k in (0, 1, 2)}
+    pair, tr = T.pair(Q), P.transposed(Q, col, 1104)
+    for a, n in PARTS:
+        rows = slice(a, a + n)
+        for k in (0, 1, 2):
+            assert torch.equal(P.plain(Q, k, rows=rows), full[k][rows]), (a, n, k)
+        assert torch.equal(T.pair(Q, rows=rows), pair[rows]), (a, n)
+        assert torch.equal(P.transposed(Q, col, up(n, 8), rows=rows)[:, :n], tr[:, rows]), (a, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("work", [True, False])
+def test_longest_sum_on_8_wave_tiles_and_in_shares(torch, Q, work):
+    """Every code -128 at the largest K, in 4 shares (sums of 2^14 K / 4 that meet in 32 bits) and unsplit, and at 15360 on an 8-wave tile."""
+    for M, N, K in ((128, 2176, Q.MAX_K), (500, 4096, 15360)):
+        P = Product(torch, M, N, K)
+        P.A.fill_(-128)
+        P.W.fill_(-128)
+        P.W[1, ::2] = 127
+        P.sa.fill_(1.0)
+        P.sw.fill_(1.0)
+        out = P.plain(Q, 1, bias=False, work=work)[:, :N]
+        some = torch.ones(N, dtype=torch.bool, device="cuda")
+        some[1] = False
+        assert bool((out[:, some] == 16384.0 * K).all()) and bool((out[:, 1] == float(np.float32(128 * 128 * (K // 2) - 128 * 127 * (K // 2)))).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[500, 500, 500, 293], [500, 500, 500, 500, 48]])
+def test_encoder_where_the_first_launch_ends_with_the_keys(torch, Q, lens):
+    """1793 and 2048 tokens at T5-XXL widths: the query, key and value product's second launch is all transposed columns."""
+    arch = dict(synth.ENCODERS["t5_xxl"], n_layers=1, vocab=512)
+    m = Q.EncoderI8(arch)
+    m.ensure_workspace(lens)
+    m.workspace.fill_(0xFF)
+    m.init_weights(7, 0.02)
+    m.quantize()
+    tok = torch.from_numpy(np.concatenate(synth.make_tokens(lens, arch["vocab"]))).cuda()
+    out = torch.full((sum(lens), arch["d_model"]), float("nan"), device="cuda")
+    m.forward(lens, tok, None, out)
+    assert bool(torch.isfinite(out).all())
+    at = 0
+    for L in lens:
+        solo = torch.full((L, arch["d_model"]), float("nan"), device="cuda")
+        m.ensure_workspace([L])
+        m.forward([L], tok[at:], None, solo)
+        torch.cuda.synchronize()
+        assert torch.equal(solo, out[at:at + L]), L
+        at += L
+    m.close()
