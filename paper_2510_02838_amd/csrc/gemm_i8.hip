@@ -30,7 +30,10 @@ __device__ __forceinline__ float gelu(float x) {
   const float e = __builtin_amdgcn_exp2f(-2.8853900817779268f * t);
   return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
-__device__ __forceinline__ float value(int acc, float sa, float sw, float bias) { return __builtin_fmaf((float)acc, sa * sw, bias); }
+// The sum times the row's scale first: two scales of the row operators, down to 2^-126 each, leave the range of float32 when multiplied with each
+// other, a sum of at least 1 times one of them does not fall below it.  Above, sum * sa has to stay under 2^128; taking the smaller scale
+// first, which would lift that too, costs 2 to 8 % (8192 x 8192 x 1024 to bf16 76.6 -> 79.5 us, of GELU 91.7 -> 97.3).
+__device__ __forceinline__ float value(int acc, float sa, float sw, float bias) { return __builtin_fmaf((float)acc * sa, sw, bias); }
 
 // four neighbouring values of a vector at any place, those past the end are 0
 typedef f32x4 f32x4_any __attribute__((aligned(4)));

@@ -182,3 +182,32 @@ def test_encoder_where_the_first_launch_ends_with_the_keys(torch, Q, lens):
         assert torch.equal(solo, out[at:at + L]), L
         at += L
     m.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(3, 300, 256), (130, 37535, 128), (1137, 4096, 256), (500, 4096, 10240)])
+def test_scales_whose_product_leaves_float32(torch, Q, M, N, K):
+    """Two legal scales may have a product below the smallest normal number or above the largest; the result need not."""
+    P = Product(torch, M, N, K, pair=True)
+    P.A.clamp_(min=1)                                                # sums of at least K
+    P.W.clamp_(min=1)
+    P.W2.clamp_(min=1)
+    u, w = P.sa / 0.01, P.sw * 50.0 * K ** 0.5                       # 0.5 .. 1.5
+    col = torch.arange(M, dtype=torch.int32, device="cuda")
+    for ea, ew in ((-80, -60), (-60, -80), (-126, 100), (80, -120)):
+        P.sa, P.sw = torch.ldexp(u, torch.tensor(ea)).clamp_min(2.0 ** -126), torch.ldexp(w, torch.tensor(ew))
+        p = P.exact()
+        # sum to float32, two products; of these the last may be below 2^-126 (130 x 37535 x 128), where float32 numbers are the multiples
+        # of 2^-149 and bf16 ones those of 2^-133, so that a rounding is off by up to half of that
+        tol = 3.01 * F32 * p + 2.0 ** -150
+        close(P.plain(Q, 1, bias=False)[:, :N], p, tol)
+        tol = tol + BF16 * (p + tol) + 2.0 ** -134
+        close(P.plain(Q, 0, bias=False)[:, :N], p, tol)
+        close(P.transposed(Q, col, up(M, 8), bias=False)[:, :M].t(), p, tol)
+    P.A.zero_()
+    P.sa, P.sw = torch.ldexp(u, torch.tensor(70)), torch.ldexp(w, torch.tensor(70))
+    P.sw2 = P.sw
+    for kind in (0, 1, 2):
+        assert bool((P.plain(Q, kind, bias=False)[:, :N] == 0.0).all())
+        assert torch.equal(P.plain(Q, 1)[:, :N], P.bias.expand(M, N))
+    assert bool((P.pair(Q)[:, :N] == 0.0).all()) and bool((P.transposed(Q, col, up(M, 8), bias=False)[:, :M] == 0.0).all())
