@@ -486,6 +486,7 @@ dit_status enc_i8_quantize(enc_ctx* c, void* dev_codes, size_t bytes) {
 static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* tokens, void* out_bf16, float* out_f32) {
   const enc_config& g = c->cfg;
   EHIP(c, hipSetDevice(c->device));
+  c->launch_refused = false;
   // the previous call's host image must have been consumed before it is rebuilt
   if (c->meta_done) EHIP(c, hipEventSynchronize(c->meta_done));
   else EHIP(c, hipEventCreateWithFlags(&c->meta_done, hipEventDisableTiming));
@@ -514,6 +515,7 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
     p.partial = (int*)(ws + L.partial); p.partial_bytes = L.partial_bytes;
     return p;
   };
+  auto launch = [&](GemmI8& p) { if (!launch_gemm_i8(s, p)) c->launch_refused = true; };   // reported by the call
 
   launch_embed_gather(s, tokens, Wv(c, "embed"), x, M, d, g.vocab);
   launch_rel_bias_table(s, Wv(c, "rel_bias"), bias, H, L.bias_L);
@@ -526,7 +528,7 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
     if (l) ETAP("l" + std::to_string(l - 1) + ".x_out", x, (size_t)M * d * 4);
     GemmI8 qkv = product(h, d, hs, at, k.qkv, k.s_qkv, 3 * inner, OUT_BF16, qk, 2 * inner);
     qkv.vt_from = 2 * inner; qkv.vt = vt; qkv.ldvt = L.base.cols_pad; qkv.vt_col = (const int*)(meta + L.base.o_vt_col);
-    launch_gemm_i8(s, qkv);
+    launch(qkv);
     AttnArgs a;
     a.q = qk; a.ldq = 2 * inner; a.k = qk + inner; a.ldk = 2 * inner; a.vt = vt; a.ldvt = L.base.cols_pad; a.o = o; a.ldo = inner;
     a.n_heads = H; a.head_dim = dh; a.cu_q = a.cu_k = (const int*)(meta + L.base.o_cu); a.vt_off = (const int*)(meta + L.base.o_vt_off);
@@ -537,21 +539,22 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
     ETAP(p + ".attn", o, (size_t)M * inner * 2);
     launch_quantize_i8(s, o, false, inner, M, inner, q8, inner, qs);
     GemmI8 po = product(q8, inner, qs, at, k.o, k.s_o, d, OUT_BF16, delta, d);
-    launch_gemm_i8(s, po);
+    launch(po);
     launch_rmsnorm_i8(s, x, d, delta, false, d, Wv(c, p + ".ln2.g"), 1e-6f, M, d, x, d, h, d, hs);
     ETAP(p + ".x_attn", x, (size_t)M * d * 4);
     GemmI8 in = product(h, d, hs, at, k.wi0, k.s_wi0, ff, OUT_BF16, act, ff);
     in.W2 = (const int8_t*)at + k.wi1; in.sw2 = (const float*)(at + k.s_wi1);
-    launch_gemm_i8(s, in);
+    launch(in);
     ETAP(p + ".act", act, (size_t)M * ff * 2);
     launch_quantize_i8(s, act, false, ff, M, ff, q8, ff, qs);
     // the next layer's norm adds the branch; the last one goes straight into the residual
     const bool last = l + 1 == g.n_layers;
     GemmI8 out = product(q8, ff, qs, at, k.wo, k.s_wo, d, last ? OUT_RESID_F32 : OUT_BF16, last ? (void*)x : (void*)delta, d);
-    launch_gemm_i8(s, out);
+    launch(out);
     if (last) ETAP(p + ".x_out", x, (size_t)M * d * 4);
   }
   launch_rmsnorm(s, x, Wv(c, "final.g"), (bf16_t*)out_bf16, out_f32, M, d);
+  if (c->launch_refused) return efail(c, DIT_ESHAPE, "a matrix product of this call is outside the GEMM kernels' limits");
   EHIP(c, hipGetLastError());
   return DIT_OK;
 }

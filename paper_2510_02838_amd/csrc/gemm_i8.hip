@@ -1035,13 +1035,12 @@ size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {
   return c.splits == 1 ? 0 : (size_t)((M + 127) / 128) * (((pair ? 2 * n : n) + 127) / 128) * c.splits * (128 * 128 * 4);
 }
 
-void launch_gemm_i8(hipStream_t s, GemmI8& p) {
+bool launch_gemm_i8(hipStream_t s, GemmI8& p) {
   const Plan plan = make_plan(p.M, p.N, p.K, p.W2 != nullptr, p.partial ? p.partial_bytes : 0);
   const int n1 = plan.first;
   if (!n1) {
     p.splits = plan.main.splits;
-    launch_gemm_i8_variant(s, p, plan.main.variant);
-    return;
+    return launch_gemm_i8_variant(s, p, plan.main.variant);
   }
   GemmI8 a = p, b = p;                                   // columns 0 .. n1 - 1, and the rest
   a.N = n1; a.splits = 1;
@@ -1054,8 +1053,7 @@ void launch_gemm_i8(hipStream_t s, GemmI8& p) {
   if (b.out) b.out = (char*)b.out + (size_t)n1 * (p.kind == OUT_F32 || p.kind == OUT_RESID_F32 ? 4 : 2);
   if (p.vt_from < n1) { b.vt += (size_t)(n1 - p.vt_from) * p.ldvt; b.vt_from = 0; }
   else b.vt_from = p.vt_from - n1;
-  launch_gemm_i8_variant(s, a, plan.main.variant);
-  launch_gemm_i8_variant(s, b, plan.rest.variant);
+  return launch_gemm_i8_variant(s, a, plan.main.variant) && launch_gemm_i8_variant(s, b, plan.rest.variant);
 }
 
 }  // namespace dit

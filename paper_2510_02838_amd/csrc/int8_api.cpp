@@ -74,8 +74,7 @@ dit_status dit_op_gemm_i8(void* stream, const void* A, int lda, const float* a_s
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W, ldw, w_scale, bias, M, N, K, out_kind, out, ldc, work, work_bytes);
   if (out_kind == OUT_RESID_F32) { p.gate = gate; p.gate_stride = gate_stride; p.row_req = row_req; }
-  launch_gemm_i8((hipStream_t)stream, p);
-  return launched();
+  return launch_gemm_i8((hipStream_t)stream, p) ? launched() : DIT_ESHAPE;
 }
 
 dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const float* a_scale, const void* W_gate, const float* gate_scale,
@@ -88,8 +87,7 @@ dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const floa
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W_gate, ldw, gate_scale, nullptr, M, N, K, OUT_BF16, out, ldc, work, work_bytes);
   p.W2 = (const int8_t*)W_up; p.sw2 = up_scale;
-  launch_gemm_i8((hipStream_t)stream, p);
-  return launched();
+  return launch_gemm_i8((hipStream_t)stream, p) ? launched() : DIT_ESHAPE;
 }
 
 dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const float* a_scale, const void* W, int ldw,
@@ -102,8 +100,7 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
   if (M == 0 || N == 0) return DIT_OK;
   GemmI8 p = product(A, lda, a_scale, W, ldw, w_scale, bias, M, N, K, OUT_BF16, nullptr, 0, work, work_bytes);
   p.vt = (bf16_t*)out; p.ldvt = ldo; p.vt_col = col; p.vt_from = 0;
-  launch_gemm_i8((hipStream_t)stream, p);
-  return launched();
+  return launch_gemm_i8((hipStream_t)stream, p) ? launched() : DIT_ESHAPE;
 }
 
 static bool sizes_ok(int M, int N, int K) { return M > 0 && N > 0 && K > 0 && K % 128 == 0 && K <= DIT_I8_MAX_K && countable(M, N); }

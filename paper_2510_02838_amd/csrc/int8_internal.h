@@ -24,7 +24,7 @@ struct GemmI8 {
   int* partial; size_t partial_bytes; // scratch for the sums of a product split along K, or null
   int tiles_m, tiles_n, splits;       // filled by the launcher
 };
-void launch_gemm_i8(hipStream_t s, GemmI8& p);
+bool launch_gemm_i8(hipStream_t s, GemmI8& p);                  // false: its choice is no variant, and the result not all written
 size_t gemm_i8_work_bytes(int M, int N, int K, bool pair);      // scratch of its choice
 // its choice of tile with so much scratch (host only): the tile; out: shares of K, columns of a first launch (0: one launch for all), and
 // the tile of the rest

@@ -1,5 +1,9 @@
 """Products of codes in shares of K, in two launches, and transposed on every tile: the calls that the shapes of test_int8.py do not
 reach.  Each list says what its shapes take, and a host test holds it to that."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -43,6 +47,45 @@ def test_the_shapes_take_what_their_lists_say(Q):
     assert shares(Q, 1100, 1030, 20480, 1) == (1, 0) and {shares(Q, n, 1030, 20480, 1)[0] for _, n in PARTS} == {1, 2, 3, 4}
     # the encoder's query, key and value product at T5-XXL widths: 1793 tokens, where the first launch ends with the keys
     assert shares(Q, 1793, 3 * 4096, 4096, 0) == (1, 2 * 4096)
+
+
+def refusing(tmp_path, body, **env):
+    """Runs a child process whose launcher of a tile knows none of them."""
+    src, so, child = tmp_path / "refuse.cpp", tmp_path / "librefuse.so", tmp_path / "child.py"
+    src.write_text("struct ihipStream_t;\nnamespace dit { struct GemmI8; bool launch_gemm_i8_variant(ihipStream_t*, GemmI8&, int) { return false; } }\n")
+    subprocess.run(["g++", "-shared", "-fPIC", str(src), "-o", str(so)], check=True)
+    child.write_text(f"import ctypes, torch, synth\nctypes.CDLL({str(so)!r}, mode=ctypes.RTLD_GLOBAL)\nfrom paper_2510_02838_amd import int8 as Q, binding as B\n" + body)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, str(child)], env=dict(os.environ, PYTHONPATH=root, **env), cwd=root, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_a_tile_that_is_not_built_fails_the_product(tmp_path):
+    """The choice offers built tiles only; if it ever does not, a call must not return DIT_OK with nothing written.  (Nothing is launched.)"""
+    refusing(tmp_path, """
+for M, N, K in ((4, 64, 128), (500, 4096, 10240), (2744, 12288, 128)):       # one launch, shares, two launches
+    got = [Q.dit_op_gemm_i8(None, 256, K, 256, 256, K, 256, None, M, N, K, 0, 256, N, None, 0, None, 256, 1 << 25),
+           Q.dit_op_gemm_i8_geglu(None, 256, K, 256, 256, 256, 256, 256, K, M, N, K, 256, N, 256, 1 << 25),
+           Q.dit_op_gemm_i8_transposed(None, 256, K, 256, 256, K, 256, None, M, N, K, 256, 4096, 256, 256, 1 << 25)]
+    assert got == [2, 2, 2], got
+""", HIP_VISIBLE_DEVICES="")                                          # (no device: the addresses are none)
+
+
+@pytest.mark.gpu
+def test_a_tile_that_is_not_built_fails_the_encoder(tmp_path):
+    refusing(tmp_path, """
+torch.cuda.set_device(0)
+m = Q.EncoderI8(synth.ENCODERS["t5_tiny"])
+m.ensure_workspace([9]); m.workspace.zero_(); m.init_weights(1, 0.05); m.quantize()
+out = torch.empty((9, synth.ENCODERS["t5_tiny"]["d_model"]), device="cuda")
+try:
+    m.forward([9], torch.zeros(9, dtype=torch.int32, device="cuda"), None, out)
+    got = 0
+except B.DitError as e:
+    got = e.status
+torch.cuda.synchronize()
+assert got == 2, got
+""")
 
 
 def close(got, want, tol):
