@@ -210,7 +210,7 @@ Codes codes_of_layer(const enc_config& g) {
 
 // bias_L: rounded up to whole tiles of 64 keys, so that the pad keys of a sequence's last tile have a place of their own in the bias
 // table too and what they round away does not depend on the longest sequence of the call.
-struct Layout8 { Layout base; int bias_L; size_t x, h, hs, qk, vt, o, q, qs, delta, act, bias, partial, partial_bytes, total; };
+struct Layout8 { Layout base; int bias_L; size_t x, h, hs, qk, vt, o, q, qs, delta, act, bias, partial, total; };
 void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector<unsigned char>* meta) {
   const enc_config& g = c->cfg;
   plan(c, n_seq, lens, L.base, meta);
@@ -227,10 +227,9 @@ void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector
   L.act = take(M * ff * 2);
   L.bias_L = (int)rup(L.base.L, 64);
   L.bias = take((size_t)g.n_heads * (2 * (size_t)L.bias_L - 1) * 4);
-  auto scratch = [&](size_t N, size_t K, bool pair) { L.partial_bytes = std::max(L.partial_bytes, gemm_i8_work_bytes((int)M, (int)N, (int)K, pair)); };
-  L.partial_bytes = 0;
-  scratch(3 * inner, d, false); scratch(d, inner, false); scratch(ff, d, true); scratch(d, ff, false);
-  L.partial = take(L.partial_bytes);
+  // (the most that the choice of any product takes, 256 shares of a tile: what the sizes of the call ask for comes and goes with them, and a
+  // workspace for a longer call would not do for a shorter one)
+  L.partial = take(PARTIAL_BYTES);
   L.total = o;
 }
 
@@ -512,7 +511,7 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
     GemmI8 p = {};
     p.A = A; p.lda = K; p.sa = sa; p.W = (const int8_t*)at + codes; p.ldw = K; p.sw = (const float*)(at + scales);
     p.M = M; p.N = N; p.K = K; p.kind = kind; p.out = out; p.ldc = ldc; p.vt_from = N;
-    p.partial = (int*)(ws + L.partial); p.partial_bytes = L.partial_bytes;
+    p.partial = (int*)(ws + L.partial); p.partial_bytes = PARTIAL_BYTES;
     return p;
   };
   auto launch = [&](GemmI8& p) { if (!launch_gemm_i8(s, p)) c->launch_refused = true; };   // reported by the call

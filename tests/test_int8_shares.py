@@ -49,6 +49,16 @@ def test_the_shapes_take_what_their_lists_say(Q):
     assert shares(Q, 1793, 3 * 4096, 4096, 0) == (1, 2 * 4096)
 
 
+def test_a_workspace_for_a_longer_call_does_for_a_shorter_one(Q):
+    """(The products of 401 to 512 tokens split at these widths, those of 513 do not.)"""
+    m = Q.EncoderI8(synth.ENCODERS["t5_xxl"], bind=False)
+    one = [m.workspace_bytes([n]) for n in range(1, 1025)]
+    many = [m.workspace_bytes([256] * k) for k in range(1, 40)]
+    assert all(a <= b for w in (one, many) for a, b in zip(w, w[1:]))
+    assert one[511] < one[512] and 0 < one[0]
+    m.close()
+
+
 def refusing(tmp_path, body, **env):
     """Runs a child process whose launcher of a tile knows none of them."""
     src, so, child = tmp_path / "refuse.cpp", tmp_path / "librefuse.so", tmp_path / "child.py"
