@@ -66,8 +66,8 @@ dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const
 
 /* Scratch that the library's choice for a product uses (pair != 0: dit_op_gemm_i8_geglu), and the tile that it takes given so much:
  * 100 * row tiles + column tiles, of 16, of a workgroup whose waves share K, or rows * 1000 + columns of an 8-wave one.  plan (may be
- * NULL) receives three numbers: the shares of K; the columns that a first launch takes where the rest has a tile of its own, else 0;
- * that tile.  Host only; 0 and -1 for sizes that the products refuse. */
+ * NULL) receives three numbers: the shares of K, where there are two launches those of the second (the first has none); the columns that a first
+ * launch takes where the rest has a tile of its own, else 0; that tile.  Host only; 0 and -1 for sizes that the products refuse. */
 size_t dit_op_gemm_i8_work_bytes(int M, int N, int K, int pair);
 int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* plan);
 

@@ -1025,7 +1025,7 @@ bool launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant) {
 
 int gemm_i8_plan(int M, int N, int K, bool pair, size_t scratch, int (&out)[3]) {
   const Plan p = make_plan(M, N, K, pair, scratch);
-  out[0] = p.main.splits; out[1] = p.first; out[2] = p.rest.variant;
+  out[0] = p.first ? p.rest.splits : p.main.splits; out[1] = p.first; out[2] = p.rest.variant;     // (a first launch has whole tiles)
   return p.main.variant;
 }
 size_t gemm_i8_work_bytes(int M, int N, int K, bool pair) {

@@ -26,8 +26,8 @@ struct GemmI8 {
 };
 bool launch_gemm_i8(hipStream_t s, GemmI8& p);                  // false: its choice is no variant, and the result not all written
 size_t gemm_i8_work_bytes(int M, int N, int K, bool pair);      // scratch of its choice
-// its choice of tile with so much scratch (host only): the tile; out: shares of K, columns of a first launch (0: one launch for all), and
-// the tile of the rest
+// its choice of tile with so much scratch (host only): the tile; out: shares of K (of the rest where there is one), columns of a first
+// launch (0: one launch for all), and the tile of the rest
 int gemm_i8_plan(int M, int N, int K, bool pair, size_t scratch, int (&out)[3]);
 // a launch with a given tile and p.splits (false: no such variant)
 bool launch_gemm_i8_variant(hipStream_t s, GemmI8& p, int variant);

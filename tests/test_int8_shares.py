@@ -49,6 +49,17 @@ def test_the_shapes_take_what_their_lists_say(Q):
     assert shares(Q, 1793, 3 * 4096, 4096, 0) == (1, 2 * 4096)
 
 
+def test_the_plan_says_the_shares_of_whichever_launch_has_them(Q):
+    plan = (Q.C.c_int * 3)()
+    for pair, tables in ((0, (SHARED, SHARED_REST)), (1, (SHARED_PAIRS, SHARED_REST_PAIRS))):
+        for table in tables:
+            for s, (n, first) in table.items():
+                Q.dit_op_gemm_i8_tile(*s, pair, SCRATCH, plan)
+                assert list(plan[:2]) == [n, first]
+                Q.dit_op_gemm_i8_tile(*s, pair, 0, plan)             # (without scratch there are none)
+                assert plan[0] == 1
+
+
 def test_a_workspace_for_a_longer_call_does_for_a_shorter_one(Q):
     """(The products of 401 to 512 tokens split at these widths, those of 513 do not.)"""
     m = Q.EncoderI8(synth.ENCODERS["t5_xxl"], bind=False)
