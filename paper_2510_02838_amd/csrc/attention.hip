@@ -213,17 +213,17 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DH == 64 ? 3 : 2) : 1) void att
     }
     if constexpr (MODE == 3) {
       // additive bias by relative position (key - query), read from the per-head table.
-      // Register e of tile t holds key  kt*64 + 32t + 16*(e/8) + 8*half + e%8.
+      // Register e of tile t holds key  kt*64 + 32t + 16*(e/8) + 8*half + e%8.  Keys past the end take the last key's bias as they take its
+      // row: with that of their own place, of any size above the real keys', they would raise the max and leave of the row sum, once their
+      // share is taken out again, rounding errors (15 more for the keys behind a query: no finite result).
       const float* bh = a.bias + (size_t)head * (2 * a.bias_L - 1);
-      const int top = 2 * a.bias_L - 2;
+      const int last = klen - 1, q_at = a.bias_L - 1 - qi;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int key = kt * KT + 32 * t + 16 * (e >> 3) + 8 * half + (e & 7);
-          int idx = key - qi + a.bias_L - 1;
-          idx = idx < 0 ? 0 : (idx > top ? top : idx);     // keys past the end are clamped copies, masked later
-          st[t][e] += bh[idx];
+          st[t][e] += bh[(uint32_t)((key < last ? key : last) + q_at)];
         }
     }
   };
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DH == 64 ? 3 : 2) : 1) void att
     step(kt, sc, sn);
     if (kt + 1 < n_kt) step(kt + 1, sn, sc);
   }
-  // Keys past the end of the segment in the last tile are copies of the last key (clamped loads): they cannot
+  // Keys past the end of the segment in the last tile are copies of the last key (clamped loads, and its bias): they cannot
   // raise the max and their V^T columns are zero, so O is unaffected; only their share of the row sum has to be
   // taken out again: the same exponentials once more (rounded to bf16 where the sums are those of the rounded
   // values).  Register e of tile t holds key  kt*64 + 32t + 16*(e/8) + 8*half + e%8.

@@ -208,9 +208,7 @@ Codes codes_of_layer(const enc_config& g) {
   return c;
 }
 
-// bias_L: rounded up to whole tiles of 64 keys, so that the pad keys of a sequence's last tile have a place of their own in the bias
-// table too and what they round away does not depend on the longest sequence of the call.
-struct Layout8 { Layout base; int bias_L; size_t x, h, hs, qk, vt, o, q, qs, delta, act, bias, partial, total; };
+struct Layout8 { Layout base; size_t x, h, hs, qk, vt, o, q, qs, delta, act, bias, partial, total; };
 void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector<unsigned char>* meta) {
   const enc_config& g = c->cfg;
   plan(c, n_seq, lens, L.base, meta);
@@ -225,8 +223,7 @@ void plan8(const enc_ctx* c, int n_seq, const int* lens, Layout8& L, std::vector
   L.q = take(M * std::max(inner, ff)); L.qs = take(M * 4);        // codes of the attention's output, then of the gated activation
   L.delta = take(M * d * 2);
   L.act = take(M * ff * 2);
-  L.bias_L = (int)rup(L.base.L, 64);
-  L.bias = take((size_t)g.n_heads * (2 * (size_t)L.bias_L - 1) * 4);
+  L.bias = take((size_t)g.n_heads * (2 * (size_t)L.base.L - 1) * 4);
   // (the most that the choice of any product takes, 256 shares of a tile: what the sizes of the call ask for comes and goes with them, and a
   // workspace for a longer call would not do for a shorter one)
   L.partial = take(PARTIAL_BYTES);
@@ -517,7 +514,7 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
   auto launch = [&](GemmI8& p) { if (!launch_gemm_i8(s, p)) c->launch_refused = true; };   // reported by the call
 
   launch_embed_gather(s, tokens, Wv(c, "embed"), x, M, d, g.vocab);
-  launch_rel_bias_table(s, Wv(c, "rel_bias"), bias, H, L.bias_L);
+  launch_rel_bias_table(s, Wv(c, "rel_bias"), bias, H, L.base.L);
   // (pad columns of the transposed values: no product writes them)
   launch_fill_u16(s, vt, (long long)inner * L.base.cols_pad, 0);
   for (int l = 0; l < g.n_layers; ++l) {
@@ -533,7 +530,7 @@ static dit_status forward_i8(enc_ctx* c, int n_seq, const int* lens, const int* 
     a.n_heads = H; a.head_dim = dh; a.cu_q = a.cu_k = (const int*)(meta + L.base.o_cu); a.vt_off = (const int*)(meta + L.base.o_vt_off);
     a.tiles = (const AttnTile*)(meta + L.base.o_tiles); a.n_tiles = L.base.n_tiles; a.q_per_tile = 128; a.o_row_map = nullptr;
     a.scale_log2 = 1.4426950408889634f;      // scores are not divided by sqrt(head_dim) in this encoder
-    a.mode = 3; a.bias = bias; a.bias_L = L.bias_L;
+    a.mode = 3; a.bias = bias; a.bias_L = L.base.L;
     launch_attention(s, a);
     ETAP(p + ".attn", o, (size_t)M * inner * 2);
     launch_quantize_i8(s, o, false, inner, M, inner, q8, inner, qs);
