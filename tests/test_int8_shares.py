@@ -275,3 +275,20 @@ def test_scales_whose_product_leaves_float32(torch, Q, M, N, K):
         assert bool((P.plain(Q, kind, bias=False)[:, :N] == 0.0).all())
         assert torch.equal(P.plain(Q, 1)[:, :N], P.bias.expand(M, N))
     assert bool((P.pair(Q)[:, :N] == 0.0).all()) and bool((P.transposed(Q, col, up(M, 8), bias=False)[:, :M] == 0.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("int8", [False, True])
+def test_stage_table_counts_the_weights_that_are_held(capsys, monkeypatch, int8):
+    """The codes come on top of the bf16 arena, which stays bound."""
+    import json
+    from paper_2510_02838_amd import encoder, int8 as Q, stage_profile
+    m = Q.EncoderI8(synth.ENCODERS["t5_tiny"], bind=False)
+    bf16, codes = encoder.Encoder.weight_bytes(m), m.code_bytes()
+    m.close()
+    monkeypatch.setattr(sys, "argv", ["stage_profile", "encode", "--encoder", "t5_tiny", "--lens", "32", "--max-batch", "2"] + ["--int8"] * int8)
+    stage_profile.main()
+    rows = [json.loads(line) for line in capsys.readouterr().out.splitlines()]
+    rows = [r for r in rows if r["table"] == "encode"]
+    assert len(rows) == 2 and all(r["weight_bytes"] == bf16 + codes * int8 and r["products"] == ("int8" if int8 else "bf16") for r in rows)
+    assert all(abs(r["weight_read_floor_ms"] - (codes if int8 else bf16) / 8e9) <= 1e-12 for r in rows)
