@@ -35,8 +35,9 @@ dit_status dit_op_quantize_i8(void* stream, const void* x, int x_kind, int ldx, 
 /* RMS norm with the residual's addition, leaving codes:
  *     x' = x + delta;   y = x' / sqrt(mean(x'^2) + eps) * gain;   codes and scales of the rows y (never rounded before).
  * x: dev float32 [M][ldx]; delta: [M][ldd], delta_kind DIT_X_*, NULL = none; x_out: dev float32 [M][ldo] receives x', may be x
- * itself (with ldo == ldx) or NULL; gain: dev float32 [d], 16-byte aligned; eps > 0; codes and columns past d as above.  The statistics are held in 64 bits, so
- * that codes and scales are those of the formulas whatever the order of the sums. */
+ * itself (with ldo == ldx) or NULL; gain: dev float32 [d], 16-byte aligned; 0 < eps <= 1e30; codes and columns past d as above.  Everything behind x' is held
+ * in 64 bits: a scale is the formula's or, where that lies within 2^-46 of itself of the middle of two float32 numbers, its neighbour, and a code is off by
+ * one at most where the quotient lies within 2^-39 of the border of two.  A row gets the same codes and scale, bit for bit, among any others. */
 dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* delta, int delta_kind, int ldd, const float* gain,
                              float eps, int M, int d, float* x_out, int ldo, void* codes, int ldq, float* scale);
 
@@ -58,7 +59,7 @@ dit_status dit_op_gemm_i8_geglu(void* stream, const void* A, int lda, const floa
                                 const void* W_up, const float* up_scale, int ldw, int M, int N, int K, void* out, int ldc,
                                 void* work, size_t work_bytes);
 
-/* bf16 of the product (+ bias), element (m, n) to out[n*ldo + col[m]]; col: dev int32 [M], rising, below ldo; columns that no
+/* bf16 of the product (+ bias), element (m, n) to out[n*ldo + col[m]]; col: dev int32 [M], every one above the one before, below ldo; columns that no
  * row maps to are left alone. */
 dit_status dit_op_gemm_i8_transposed(void* stream, const void* A, int lda, const float* a_scale, const void* W, int ldw,
                                      const float* w_scale, const float* bias, int M, int N, int K, void* out, int ldo,
@@ -74,11 +75,12 @@ int dit_op_gemm_i8_tile(int M, int N, int K, int pair, size_t work_bytes, int* p
 /* ---- the Encode stage in 8 bits ------------------------------------------------------- */
 
 /* enc_forward (encoder.h) with its matrix products on codes: weights with a scale per output channel, their inputs with one per token.
- * The residual stream and the norms' statistics are as there (float32, 64 bits), attention runs on bf16, a branch is rounded to bf16 before
- * the next norm adds it (the last one is added in float32).
+ * The residual stream is float32 as there; the statistics of the layers' norms are held in 64 bits, of the final one in float32; attention runs on
+ * bf16; a branch is rounded to bf16 before the next norm adds it to the stream (the last one is added in float32), where enc_forward adds float32 sums.
  *
  * enc_i8_quantize writes the codes of every matrix of the bound weight arena to dev_codes (256-byte aligned, enc_i8_weight_bytes), which the
- * context refers to from then on; the arena stays in use (embedding, bias table, gains).  It has to be called again after
+ * context refers to from then on.  The codes come on top of the arena, which stays bound and in use (embedding, bias table, gains): this form
+ * reads half the bytes a pass and holds half as many again.  It has to be called again after
  * enc_init_weights, enc_set_tensor of a matrix and a bind of another arena, after which enc_i8_forward refuses with DIT_EINVAL, and after the
  * arena has been written by other means.
  * DIT_EUNSUPPORTED for matrices with more than DIT_I8_MAX_ROW inputs.

@@ -174,8 +174,8 @@ __device__ __forceinline__ void tile_coords(const P& p, int t, int& tm, int& tn)
 // K) are one stream, so the next tile's first slabs arrive under the epilogue.
 // Operands are swapped (W in the place of the MFMA's rows, its rows in the order {0-3, 8-11, ...}, {4-7, ...}), which gives a lane
 // 8 neighbouring columns of one row; tiles of transposed results keep the first order with the rows of A permuted.
-//   Bound: the matrix cores at the clock that the board's power leaves them.  8192^3 380 us, 2.89 POP/s, matrix cores busy in 87 % of the
-// cycles at 1.44 GHz; 8000 x 12288 x 4096 310 us as bf16, 327 as fp32.  (128x128 tiles: what a CU pulls, 32 KB in 0.36 to 0.48 us.)
+//   Bound: the matrix cores at the clock that the board's power leaves them.  8192^3 375 to 400 us, 2.75 to 2.95 POP/s, matrix cores busy in 87 %
+// of the cycles at 1.43 to 1.54 GHz; 8000 x 12288 x 4096 300 to 310 us as bf16, 330 to 340 as fp32.  (128x128 tiles: what a CU pulls, 32 KB in 0.36 to 0.48 us.)
 template <int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
   Problem& P = *(Problem*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -936,13 +936,14 @@ bool launch_stream_m(hipStream_t s, GemmI8& p, int nt) {
 // The variant with the least estimated time, in microseconds: a start, the rounds of 256 workgroups, in each the slabs of one tile and a
 // fixed part (first loads, sums of the waves, epilogue).  A slab of a stream tile takes 2 KB a row tile of what a CU pulls and a share of
 // its products; a slab of an 8-wave tile takes longer the more CUs run one (the clock falls with the matrix load: 256x256 0.7 us for
-// one, 1.2 with all of them busy, 1.3 round after round).  Nothing is faster than its bytes at 4.8 TB/s.
+// one, 1.2 with all of them busy, 1.3 round after round).  No estimate is below its bytes at 4.8 TB/s, with which the rest was fitted: weights from HBM
+// come no faster, those in the memory-side cache up to a tenth (1 x 12288 x 4096), which only levels tiles that are all as fast as their bytes.
 // The constants were fitted to 312 products of 1 to 8000 rows, 300 to 12288 columns and K from 512 to 10240 with every variant timed: the
 // one chosen took 1.005 times the best one's time in the mean, 1.09 at most; over 140 other shapes 1.013 and 1.13 (the most where a last
 // round of few tiles has a launch of its own).  Both sides near the borders: 128 rows, N = 4096, K = 4096 stream
 // 7.6, 128x128 14; 200 rows, N = 12288 128x128 20, stream 23; 333 rows, N = 4096, K = 10240 stream 22.2, 128x128 34; 500 rows, N = 12288
 // 128x256 27.8, 256x256 38.2; 1000 rows 52.7 and 44.2; 1000 rows, N = 4096 128x128 20.6, 128x256 25.4.  Two shares of K: 500 rows, N = 4096,
-// K = 10240 31.9, unsplit 36.6, stream 39.8; 248 rows, N = 6176, K = 9600 anything unsplit takes 27 % longer.
+// K = 10240 to bf16 31.9 (26.4 and the reduction's 5.5), unsplit 36.6, stream 39.8; 248 rows, N = 6176, K = 9600 anything unsplit takes 27 % longer.
 //   Columns that fill whole rounds of 256 8-wave tiles go ahead of the rest, which then takes the tile that suits it, where that saves 5 %:
 // 528 tiles are two rounds and 16 tiles more.  2744 x 12288 x 4096 138 -> 125 us, a gated pair of 1000 x 10240 x 4096 92 -> 79; without the
 // 5 % 2200 x 4096 x 10240 89 -> 94.  160 drawn shapes where it is chosen: 0.76 to 1.10 of the best 8-wave tile in one launch, 0.944 in the

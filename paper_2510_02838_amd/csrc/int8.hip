@@ -4,8 +4,8 @@
 //   norm:   x' = x + delta,  row = x' / sqrt(mean(x'^2) + eps) * gain
 //
 // One pass: a row stays in registers between its reductions and its codes.  Up to 1024 columns a wave owns a row, above a
-// workgroup does.  Bound: memory: 32000 x 10240 bf16 to codes 184 us (5.3 TB/s), 32000 x 4096 norm with a bf16 branch 259 us (5.6; a 4 GiB
-// copy reaches 4.8); a launch for few rows: 32 x 4096 norm 4.4 us, with two reductions behind each other and LDS permutations 4.7.
+// workgroup does.  Bound: memory: 32000 x 10240 bf16 to codes 197 us (5.0 TB/s), 32000 x 4096 norm with a bf16 branch 263 us (5.5; a 4 GiB
+// copy reaches 4.8); a launch for few rows: 32 x 4096 norm 4.6 us (with two reductions behind each other and LDS permutations 0.3 more).
 #include "int8_internal.h"
 
 namespace dit {
