@@ -8,40 +8,42 @@ from helpers import rel_l2
 from oracle import encoder_oracle as E
 from test_encoder_int8 import coded
 
-ARCH = synth.ENCODERS["t5_tiny"]
+ARCHS = {64: synth.ENCODERS["t5_tiny"], 128: dict(synth.ENCODERS["t5_tiny"], n_heads=2, head_dim=128)}
 B16 = lambda v: synth.round_bf16(v.astype(np.float32)).astype(np.float64)  # noqa: E731
 
 
-def attention(h, weights, bias):
+def attention(arch, h, weights, bias):
     """softmax(q k^T + bias) v of the rows h in 64 bits, from queries, keys and values as bf16."""
-    H, dh, n = ARCH["n_heads"], ARCH["head_dim"], h.shape[0]
+    H, dh, n = arch["n_heads"], arch["head_dim"], h.shape[0]
     q, k, v = (B16(h @ w).reshape(n, H, dh) for w in weights)
     return np.stack([E.softmax_rows(q[:, i] @ k[:, i].T + bias[i]) @ v[:, i] for i in range(H)], axis=1).reshape(n, H * dh)
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("int8", [False, True])
 @pytest.mark.parametrize("after", [6.0, 15.0, 40.0, -40.0])
 @pytest.mark.parametrize("lens", [[1], [40], [33, 129, 64, 7]])
-def test_keys_past_the_end_have_no_bias(int8, after, lens):
+def test_keys_past_the_end_have_no_bias(dh, int8, after, lens):
     """Keys behind a query get `after` more than those before it.  The last queries of a sequence have few or no such keys, but the places
     that fill its last tile up are all behind them: e^40 times the real ones' share, or e^6, of which float32 sums lose 2^-24
     each.  What is left of the error is the bf16 of probabilities and result, 2^-9 of each (rms)."""
     import torch
     from paper_2510_02838_amd import encoder, int8 as Q
-    params = synth.make_params(E.param_shapes(ARCH), 1, 0.05, 0.0, 0.1)
+    arch = ARCHS[dh]
+    params = synth.make_params(E.param_shapes(arch), 1, 0.05, 0.0, 0.1)
     params["embed"] = synth.round_bf16(params["embed"] / 0.05)
     params["rel_bias"] = synth.round_bf16(params["rel_bias"] / 0.05)
     params["rel_bias"][16:] = synth.round_bf16(params["rel_bias"][16:] + np.float32(after))
-    toks = synth.make_tokens(lens, ARCH["vocab"])
-    m = (Q.EncoderI8 if int8 else encoder.Encoder)(ARCH)
+    toks = synth.make_tokens(lens, arch["vocab"])
+    m = (Q.EncoderI8 if int8 else encoder.Encoder)(arch)
     m.ensure_workspace(lens)
     m.workspace.fill_(0xFF)
     m.init_weights(0, 0.0)
     m.set_params(params)
     if int8:
         m.quantize()
-    n, d, inner = sum(lens), ARCH["d_model"], ARCH["n_heads"] * ARCH["head_dim"]
+    n, d, inner = sum(lens), arch["d_model"], arch["n_heads"] * arch["head_dim"]
     ln, at = (torch.zeros((n, w), dtype=torch.bfloat16, device="cuda") for w in (d, inner))
     m.set_tap("l0.attn", at)
     if not int8:
@@ -58,7 +60,7 @@ def test_keys_past_the_end_have_no_bias(int8, after, lens):
             h, w8 = coded(E.rms_norm(p["embed"][t], p["l0.ln1.g"])), [coded(x.T).T for x in w]
         else:
             h, w8 = ln[o:o + L].double().cpu().numpy(), w
-        want, got = attention(h, w8, E.position_bias(L, p["rel_bias"])), at[o:o + L].double().cpu().numpy()
+        want, got = attention(arch, h, w8, E.position_bias(L, p["rel_bias"])), at[o:o + L].double().cpu().numpy()
         for rows in (slice(None), slice(L - max(1, L // 4), L)):
             assert rel_l2(got[rows], want[rows]) <= 1e-2, (L, rel_l2(got[rows], want[rows]))
         o += L
