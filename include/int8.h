@@ -45,8 +45,8 @@ dit_status dit_op_rmsnorm_i8(void* stream, const float* x, int ldx, const void* 
  * A: codes [M][lda]; W: codes [N][ldw] (no padding rows needed); a_scale: dev float32 [M]; w_scale: dev float32 [N]; bias: dev float32
  * [N] or NULL; K a multiple of 128, at most DIT_I8_MAX_K; lda, ldw multiples of 16 below 2^22; ldc below 2^26.  out_kind, out, ldc, gate, gate_stride and row_req
  * as for dit_op_gemm (0 bf16, 1 float32, 2 bf16 of tanh-GELU, 3 float32 out += gate * C); any code -128..127 is
- * taken.  The sum is multiplied by a_scale first, then by w_scale: a result may use the whole range of float32 as long as |sum| * a_scale stays below
- * 2^128 (rows of codes in -127 .. 127: as long as max|row of A's values| does below 2^128 / (127 K)), past that it is infinite.  The result does not depend on how the product is cut up: it is the same, bit for bit, alone or among other rows.
+ * taken.  Scales are at least 2^-126; a result may be any float32 number, whatever the product of its scales is alone.  (Save beside rows with an a_scale
+ * above 2^96: rows with one below 2^-94 may lose digits there, and the other rows' results of columns with a w_scale above 2^96 be too small.)  The result does not depend on how the product is cut up: it is the same, bit for bit, alone or among other rows.
  * work: dev scratch for the shares of a product that is split along K between workgroups (dit_op_gemm_i8_work_bytes says how much the
  * library's choice takes, for most sizes nothing); with NULL or less another tile is taken.  Its contents carry nothing between
  * calls; calls that may overlap need one each. */

@@ -31,9 +31,19 @@ __device__ __forceinline__ float gelu(float x) {
   return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
 // The sum times the row's scale first: two scales of the row operators, down to 2^-126 each, leave the range of float32 when multiplied with each
-// other, a sum of at least 1 times one of them does not fall below it.  Above, sum * sa has to stay under 2^128; taking the smaller scale
-// first, which would lift that too, costs 2 to 8 % (8192 x 8192 x 1024 to bf16 76.6 -> 79.5 us, of GELU 91.7 -> 97.3).
+// other, a sum of at least 1 times one of them does not fall below it.  (The smaller scale first costs 2 to 8 %: 8192 x 8192 x 1024 to bf16
+// 76.6 -> 79.5 us, of GELU 91.7 -> 97.3.)
 __device__ __forceinline__ float value(int acc, float sa, float sw, float bias) { return __builtin_fmaf((float)acc * sa, sw, bias); }
+// A sum, below 2^31, times a row's scale above LARGE may be past float32 where the result is not: 2^32 is moved from such a scale to the columns'
+// then, which changes no bit of a result.  (A column's scale that this takes past float32 becomes the largest number, so that a sum of 0 stays one.)
+constexpr float LARGE = 0x1p96f, LARGEST = 0x1.fffffep127f;
+__device__ __forceinline__ float eased_row(float sa, bool large) { return large ? sa * 0x1p-32f : sa; }
+__device__ __forceinline__ float eased_col(float sw, bool large) {
+  if (!large) return sw;
+  const float t = sw * 0x1p32f;
+  return t > LARGEST && sw <= LARGEST ? LARGEST : t;
+}
+__device__ __forceinline__ bool any_lane(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
 
 // four neighbouring values of a vector at any place, those past the end are 0
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
@@ -68,6 +78,16 @@ __device__ __forceinline__ Ahead fetch4(const P& p, int m, int n) {
     }
   }
   return a;
+}
+template <bool PAIR>
+__device__ __forceinline__ void ease4(Ahead& a) {
+  const bool large = a.sa > LARGE;
+  a.sa = eased_row(a.sa, large);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    a.sw[c] = eased_col(a.sw[c], large);
+    if constexpr (PAIR) a.more[c] = eased_col(a.more[c], large);
+  }
 }
 // the four results to their places; up: the same columns of a pair's second product
 template <class P>
@@ -125,7 +145,8 @@ __device__ __forceinline__ void put_col4(const P& p, int m, int n, const i32x4& 
   for (int c = 0; c < 4; ++c) {
     const int k = m + c < p.M ? m + c : m;
     col[c] = p.vt_col[k];
-    v[c] = bf(value(acc[c], p.sa[k], sw, b));
+    const bool large = p.sa[k] > LARGE;
+    v[c] = bf(value(acc[c], eased_row(p.sa[k], large), eased_col(sw, large), b));
   }
   if (m + 4 <= p.M && col[3] == col[0] + 3 && (col[0] & 3) == 0)       // (columns rise)
     *(uint2*)(dst + col[0]) = make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
@@ -388,6 +409,16 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) sa[r] = row_scale(mw + r * 16 + l16);
     };
+    // (for all rows of a lane at once, which share its columns' scales)
+    auto ease = [&](auto& rows, auto&... cols) {
+      bool large = false;
+      for (float s : rows) large |= s > LARGE;
+      if (any_lane(large)) {
+        for (float& s : rows) s = eased_row(s, large);
+        auto of = [&](auto& c) { for (float& s : c) s = eased_col(s, large); };
+        (of(cols), ...);
+      }
+    };
     auto plain_bf16 = [&](auto gelu_tag) {
       float sw[2][8], bv[2][8];
 #pragma unroll
@@ -397,6 +428,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       const int ldc = P.ldc;
       bf16_t* const out = (bf16_t*)P.out;
       const uint32_t voff = (uint32_t)(prow * ldc + pchunk * 8) * 2u;
+      ease(sa, sw[0], sw[1]);
       auto make = [&](int r, u32x4 (&w)[2]) {
         u32x4 p[2];
 #pragma unroll
@@ -482,6 +514,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       };
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) load_x(u);
+      ease(sa, sw[0], sw[1]);
       u32x4 w[2], nx[2];
       make(0, w);
 #pragma unroll
@@ -533,7 +566,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
       // All units' row scales and the columns of my pieces' rows, ahead of the stores: a load behind them waits for them to be done (pieces
       // fetched one by one where they are stored made ragged rows cost 9 us more than neighbours, so 2).
-      float sr[RT / 2][8];
+      float sr[RT * 4];
       int col[RT / 2][8];
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
@@ -543,12 +576,13 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
         if (mb + 32 <= M) {
           const f32x4 lo = *(const f32x4_any*)(P.sa + mb + kq * 8), hi = *(const f32x4_any*)(P.sa + mb + kq * 8 + 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { sr[i][e] = lo[e]; sr[i][4 + e] = hi[e]; }
+          for (int e = 0; e < 4; ++e) { sr[i * 8 + e] = lo[e]; sr[i * 8 + 4 + e] = hi[e]; }
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sr[i][e] = row_scale(mb + kq * 8 + e);
+          for (int e = 0; e < 8; ++e) sr[i * 8 + e] = row_scale(mb + kq * 8 + e);
         }
       }
+      ease(sr, sw);
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
         const int mp = mw + i * 32 + fc * 8;
@@ -560,7 +594,7 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
             const int c = cp * 2 + q;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = value(acc[2 * i + (e >> 2)][c][e & 3], sr[i][e], sw[c], bv[c]);
+            for (int e = 0; e < 8; ++e) v[e] = value(acc[2 * i + (e >> 2)][c][e & 3], sr[i * 8 + e], sw[c], bv[c]);
             const u32x4 w = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
             *(u32x4*)at(q * 16 + l16, kq) = w;
           }
@@ -590,13 +624,14 @@ __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
       const int nw2 = nw >> 1, ldc = P.ldc;
       bf16_t* const out = (bf16_t*)P.out;
       float sg[8], su[8];
+      load_sa();
       load_cols(P.sw, nw2 + kq * 8, N, sg);
       load_cols(P.sw2, nw2 + kq * 8, N, su);
-      load_sa();
       const int fr = ln >> 2, fc = ln & 3;               // my row (and the one 16 on) and piece when 32 rows are read back
       auto at = [&](int f, int chunk) { return patch + f * 64 + ((chunk ^ ((f >> 2) & 3)) << 4); };
       const bool full = nw2 + fc * 8 + 8 <= N;
       const uint32_t voff = (uint32_t)(fr * ldc + fc * 8) * 2u;
+      ease(sa, sg, su);
 #pragma unroll
       for (int i = 0; i < RT / 2; ++i) {
 #pragma unroll
@@ -694,12 +729,14 @@ __global__ __launch_bounds__(256) void reduce_i8_kernel(const GemmI8 P) {
     return s;
   };
   if (pair) {
-    const Ahead a = fetch4<true>(P, m, n);
+    Ahead a = fetch4<true>(P, m, n);
+    ease4<true>(a);
     put_pair4(P, m, n, sum(c), sum(c + 2), a);
   } else if (vt) {
     put_col4(P, m, n, sum(c));
   } else {
-    const Ahead a = fetch4<false>(P, m, n);
+    Ahead a = fetch4<false>(P, m, n);
+    ease4<false>(a);
     put_row4(P, m, n, sum(c), a);
   }
 }
@@ -872,8 +909,12 @@ __global__ __launch_bounds__((StreamShape<MT, NT, PAIR>::WV * 64)) void stream_i
       for (int u = 0; u < U; ++u) {
         if (!in[u]) continue;
         const int i = row[u] >> 4, j = g[u] >> 2, m = m0 + i0 * 16 + row[u], n = n0 + g[u] * 4;
-        if constexpr (PAIR) put_pair4(P, m, n, sum(place(i, j, row[u] & 15, g[u] & 3)), sum(place(i, j + NC, row[u] & 15, g[u] & 3)), ahead[u]);
-        else put_row4(P, m, n, sum(place(i, j, row[u] & 15, g[u] & 3)), ahead[u]);
+        const i32x4 t = sum(place(i, j, row[u] & 15, g[u] & 3));
+        i32x4 up;
+        if constexpr (PAIR) up = sum(place(i, j + NC, row[u] & 15, g[u] & 3));
+        if (any_lane(ahead[u].sa > LARGE)) ease4<PAIR>(ahead[u]);
+        if constexpr (PAIR) put_pair4(P, m, n, t, up, ahead[u]);
+        else put_row4(P, m, n, t, ahead[u]);
       }
       q0 += U * STEP;
       if (q0 >= ALL) break;

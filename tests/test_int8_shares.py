@@ -278,6 +278,52 @@ def test_scales_whose_product_leaves_float32(torch, Q, M, N, K):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(3, 300, 256), (130, 37535, 128), (176, 17220, 128), (1137, 4096, 256), (500, 4096, 10240), (333, 1000, 1536)])
+def test_scales_near_the_largest_number(torch, Q, M, N, K):
+    """Rows of numbers up to 2^128 have scales up to 2^121: a sum times one is past float32, the result need not be.  Every form, alone and beside
+    rows of ordinary size, of zeros and of 2^-90; a row's result is the same, bit for bit, without the rows beside it."""
+    P = Product(torch, M, N, K, pair=True)
+    P.A[::5] = 0
+    u, w = P.sa / 0.01, P.sw * 50.0 * K ** 0.5                       # 0.5 .. 1.5
+    P.sw = torch.ldexp(w, torch.tensor(-124))                        # (2^-126 is the smallest scale)
+    P.sw2 = P.sw.flip(0).contiguous()
+    P.bias *= 0.25
+    every = torch.arange(M, device="cuda")
+    e = torch.tensor([-126, 110, 120, 0, -90], device="cuda")[every % 5]
+    col = every.to(torch.int32)
+    b = P.bias.double()
+    for sa in (torch.ldexp(u, torch.tensor(110)), torch.ldexp(u, torch.tensor(120)), torch.ldexp(u, e).clamp_min(2.0 ** -126)):
+        P.sa = sa
+        p, p2 = P.exact(), P.exact(P.W2, P.sw2)
+        dv, d2 = 3.01 * F32 * (p.abs() + abs(b)) + 2.0 ** -150, 3.01 * F32 * p2.abs() + 2.0 ** -150     # (as above: results below 2^-126)
+        dp = 3.01 * F32 * p.abs() + 2.0 ** -150
+        v = p + b
+        out = {k: P.plain(Q, k) for k in (0, 1, 2)}
+        close(out[1][:, :N], v, dv)
+        close(out[0][:, :N], v, dv + BF16 * (v.abs() + dv) + 2.0 ** -134)
+        tr = P.transposed(Q, col, up(M, 8))
+        close(tr[:, :M].t(), v, dv + BF16 * (v.abs() + dv) + 2.0 ** -134)
+        tol = gelu_bound(v, dv)
+        close(out[2][:, :N], gelu64(v), tol + BF16 * (gelu64(v).abs() + tol) + 2.0 ** -134)
+        x = torch.randn(M, up(N, 8) + 8, generator=torch.Generator().manual_seed(2)).cuda()
+        got = P.plain(Q, 3, bias=False, out=x.clone())
+        want = x[:, :N].double() + p
+        close(got[:, :N], want, 1.01 * F32 * want.abs() + dp)
+        pair = P.pair(Q)
+        want = gelu64(p) * p2
+        tol = gelu_bound(p, dp)
+        tol = tol * p2.abs() + gelu64(p).abs() * d2 + tol * d2
+        tol = tol + (BF16 + F32) * (want.abs() + tol) + 2.0 ** -134
+        close(pair[:, :N], want, tol)
+        for a, n in ((0, 1), (1, 2), (M // 2, M - M // 2)):
+            rows = slice(a, a + n)
+            for k in (0, 1, 2):
+                assert torch.equal(P.plain(Q, k, rows=rows), out[k][rows])
+            assert torch.equal(P.pair(Q, rows=rows), pair[rows])
+            assert torch.equal(P.transposed(Q, col, up(n, 8), rows=rows)[:, :n], tr[:, rows])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("int8", [False, True])
 def test_stage_table_counts_the_weights_that_are_held(capsys, monkeypatch, int8):
     """The codes come on top of the bf16 arena, which stays bound."""
