@@ -10,7 +10,8 @@
  *   c = RMSNorm(x) g_final
  *   RMSNorm: x / sqrt(mean(x^2) + 1e-6), no mean subtraction; no biases; 32 relative-position
  *   buckets (16 per direction: distances 0..7 exact, then 8 + floor(8 ln(n/8)/ln 16), distances
- *   from 128 on share the last), one bias table [32][heads] for all layers.
+ *   from 128 on share the last), one bias table [32][heads] for all layers (biases past +-2^29, infinite ones
+ *   among them, count as +-2^29: keys to be left out may have any of the usual values for that).
  *
  * Conventions are those of dit.h (status codes, caller-owned device buffers, nothing
  * allocated by the library, errors kept per context, no CPU fallback).  Sequences are packed

@@ -130,7 +130,12 @@ __global__ __launch_bounds__(256) void rel_bias_table_kernel(const float* __rest
     for (int b = 1; b < 8; ++b) bucket += (n * n >= (64 << b)) ? 1 : 0;
   }
   if (delta > 0) bucket += 16;
-  bias[i] = table[bucket * H + h];
+  // A tile of keys that all have a very low bias gives the running max a value whose product with log2(e) is off by up to half its last place, and
+  // the probabilities that far from 1: below 2^29 a factor of 2^32, which the first key that counts takes out again; infinite from some
+  // 2^31 on, and then no number.  A key that far down counts for nothing either way.
+  const float b = table[bucket * H + h];
+  constexpr float MOST = 0x1p29f;
+  bias[i] = b > MOST ? MOST : b < -MOST ? -MOST : b;       // (a NaN stays one)
 }
 
 void launch_rel_bias_table(hipStream_t s, const float* table, float* bias, int H, int L) {

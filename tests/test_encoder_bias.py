@@ -19,22 +19,16 @@ def attention(arch, h, weights, bias):
     return np.stack([E.softmax_rows(q[:, i] @ k[:, i].T + bias[i]) @ v[:, i] for i in range(H)], axis=1).reshape(n, H * dh)
 
 
-@pytest.mark.gpu
-@pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("int8", [False, True])
-@pytest.mark.parametrize("after", [6.0, 15.0, 40.0, -40.0])
-@pytest.mark.parametrize("lens", [[1], [40], [33, 129, 64, 7]])
-def test_keys_past_the_end_have_no_bias(dh, int8, after, lens):
-    """Keys behind a query get `after` more than those before it.  The last queries of a sequence have few or no such keys, but the places
-    that fill its last tile up are all behind them: e^40 times the real ones' share, or e^6, of which float32 sums lose 2^-24
-    each.  What is left of the error is the bf16 of probabilities and result, 2^-9 of each (rms)."""
+def check(dh, int8, lens, change):
+    """The first layer's attention against softmax(q k^T + bias) v.  What is left of the error is the bf16 of probabilities and
+    result, 2^-9 of each (rms)."""
     import torch
     from paper_2510_02838_amd import encoder, int8 as Q
     arch = ARCHS[dh]
     params = synth.make_params(E.param_shapes(arch), 1, 0.05, 0.0, 0.1)
     params["embed"] = synth.round_bf16(params["embed"] / 0.05)
     params["rel_bias"] = synth.round_bf16(params["rel_bias"] / 0.05)
-    params["rel_bias"][16:] = synth.round_bf16(params["rel_bias"][16:] + np.float32(after))
+    change(params["rel_bias"])
     toks = synth.make_tokens(lens, arch["vocab"])
     m = (Q.EncoderI8 if int8 else encoder.Encoder)(arch)
     m.ensure_workspace(lens)
@@ -65,3 +59,29 @@ def test_keys_past_the_end_have_no_bias(dh, int8, after, lens):
             assert rel_l2(got[rows], want[rows]) <= 1e-2, (L, rel_l2(got[rows], want[rows]))
         o += L
     m.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("after", [6.0, 15.0, 40.0, -40.0])
+@pytest.mark.parametrize("lens", [[1], [40], [33, 129, 64, 7]])
+def test_keys_past_the_end_have_no_bias(dh, int8, after, lens):
+    """Keys behind a query get `after` more than those before it.  The last queries of a sequence have few or no such keys, but the places
+    that fill its last tile up are all behind them: e^40 times the real ones' share, or e^6, of which float32 sums lose 2^-24 each."""
+    def change(table):
+        table[16:] = synth.round_bf16(table[16:] + np.float32(after))
+    check(dh, int8, lens, change)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("far", [-1e4, -1e9, -1e10, -3e38, -np.inf])
+@pytest.mark.parametrize("rows", [slice(16, 32), slice(1, 16), slice(8, 16)])
+def test_biases_that_mask(dh, int8, far, rows):
+    """No key behind a query counts, or none before it, or none more than seven places before it: whole tiles of 64 keys that count for nothing
+    come first for the later queries.  (The next layer's inputs have the same shape: the outputs stay finite.)"""
+    def change(table):
+        table[rows] = far
+    check(dh, int8, [200, 64, 65, 1], change)
