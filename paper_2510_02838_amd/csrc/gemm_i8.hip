@@ -195,8 +195,8 @@ __device__ __forceinline__ void tile_coords(const P& p, int t, int& tm, int& tn)
 // K) are one stream, so the next tile's first slabs arrive under the epilogue.
 // Operands are swapped (W in the place of the MFMA's rows, its rows in the order {0-3, 8-11, ...}, {4-7, ...}), which gives a lane
 // 8 neighbouring columns of one row; tiles of transposed results keep the first order with the rows of A permuted.
-//   Bound: the matrix cores at the clock that the board's power leaves them.  8192^3 375 to 400 us, 2.75 to 2.95 POP/s, matrix cores busy in 87 %
-// of the cycles at 1.43 to 1.54 GHz; 8000 x 12288 x 4096 300 to 310 us as bf16, 330 to 340 as fp32.  (128x128 tiles: what a CU pulls, 32 KB in 0.36 to 0.48 us.)
+//   Bound: the matrix cores at the clock that the board's power leaves them.  8192^3 370 to 400 us, 2.75 to 2.95 POP/s, matrix cores busy in 87 %
+// of the cycles at 1.36 to 1.54 GHz; 8000 x 12288 x 4096 300 to 310 us as bf16, 330 to 340 as fp32.  (128x128 tiles: what a CU pulls, 32 KB in 0.36 to 0.48 us.)
 template <int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(512) void gemm8_i8_kernel(const GemmI8) {
   Problem& P = *(Problem*)__builtin_amdgcn_kernarg_segment_ptr();
